@@ -74,7 +74,7 @@ typedef enum {
     EAD_ERR_STATE = 9           /* call order violated (e.g. ead_decode before ead_begin) */
 } ead_status;
 
-typedef enum { EAD_F32 = 0, EAD_BF16 = 1 } ead_dtype;
+typedef enum { EAD_F32 = 0, EAD_BF16 = 1, EAD_FP8 = 2 /* e4m3; the pages of a paged cache only */ } ead_dtype;
 typedef enum { EAD_MODEL_SMALL = 0, EAD_MODEL_LARGE = 1 } ead_model_id;
 typedef enum { EAD_NATS = 0, EAD_BITS = 1 } ead_unit;   /* Eq. 2 is written in bits */
 
@@ -272,6 +272,72 @@ ead_status ead_gate_run_logits(ead_gate *g, const void *const *logits_dev_list, 
                                float *window_mean_dev);
 ead_status ead_gate_reset(ead_gate *g);
 void ead_gate_destroy(ead_gate *g);
+
+/* ---- a paged cache of the caller's, and attention over it -------------------------- */
+
+/* The cache of one attention layer, in pages of the caller's device memory:
+ *   k, v              [n_pages][n_kv_heads][page_size][head_dim] of `dtype`, 16-byte aligned
+ *   k_scale, v_scale  [n_pages][n_kv_heads][page_size], EAD_FP8 only (null otherwise): the head's
+ *                     vector at that position is its e4m3 codes times 2^(scale - 127)
+ * page_size is 16, 32, 64, 128 or 256; head_dim 32, 64 or 128.  Rounding to EAD_FP8 takes the smallest
+ * power of two that brings the vector's largest finite magnitude to 448 or less, so codes times
+ * scale are exact in bf16; elements that are not finite become NaN. */
+typedef struct {
+    int32_t dtype, n_pages, page_size, n_kv_heads, head_dim;
+    void *k, *v;
+    uint8_t *k_scale, *v_scale;
+} ead_paged_cache;
+
+/* What a call works on: `batch` sequences, each with some rows (its new tokens).  Arrays are device memory.
+ *   page_table [batch][table_stride], the first table_width entries of a row are used: entry i is the
+ *              page of positions i * page_size .. + page_size.  A number outside 0 .. n_pages-1 is a hole:
+ *              nothing is written there, zeros are read from there, and attention sees nothing there
+ *   q_starts   [batch + 1]: rows q_starts[b] .. q_starts[b+1]-1 of the call's tensors are sequence b's
+ *   kv_lens    [batch]: positions the sequence holds, its rows the last of them (row i of n is position
+ *              kv_lens[b] - n + i; rows at positions below 0 are neither written nor see anything)
+ * The host says how much that is at most, which decides grids and workspaces: `rows` in all (exact),
+ * max_q / min_q rows of one sequence and max_kv positions of one.  The arrays may change between calls (a
+ * captured graph reads them anew); nothing is read or written out of range where they exceed the bounds, but
+ * rows beyond max_q may then not be computed by ead_paged_attention.  Limits: batch <= 65535, rows * heads < 2^30. */
+typedef struct {
+    int32_t batch, rows, max_q, min_q, max_kv, table_stride, table_width;
+    const int32_t *page_table, *q_starts, *kv_lens;
+} ead_paged_batch;
+
+/* A caller's tensor [rows][heads][head_dim]: strides in elements, head_dim contiguous.  Any strides and
+ * alignment to the element are taken; 16-byte aligned vectors are the faster ones. */
+typedef struct {
+    void *data;
+    int64_t row_stride, head_stride;
+} ead_rows;
+
+/* K and V of the batch's rows (`dtype` EAD_F32 or EAD_BF16) to their places in the pages, rounded to nearest
+ * even.  All three calls are asynchronous on `hip_stream`, allocate nothing and can be captured in a graph. */
+ead_status ead_paged_write(const ead_paged_cache *cache, const ead_paged_batch *batch, int32_t dtype,
+                           const ead_rows *k, const ead_rows *v, void *hip_stream);
+/* The rows' K and V back from the pages, as `dtype` (EAD_F32 or EAD_BF16).  A batch whose rows are all the
+ * positions of its sequences reads whole sequences. */
+ead_status ead_paged_read(const ead_paged_cache *cache, const ead_paged_batch *batch, int32_t dtype,
+                          const ead_rows *k, const ead_rows *v, void *hip_stream);
+
+/* Attention of the rows' queries, [rows][n_heads][head_dim] of `dtype`, over the pages: EAD_F32 over an EAD_F32
+ * cache, EAD_BF16 over an EAD_BF16 or EAD_FP8 one.  Query head h reads KV head h / (n_heads / n_kv_heads).  The row
+ * at position p sees positions j <= p, with window > 0 only those with p - j < window or j < sinks.
+ *   out = sum_j softmax_j(scale q.k_j) v_j;  lse (nullable, [rows][n_heads] float32) = ln sum_j exp(scale q.k_j)
+ * A row that sees nothing gets 0 and -infinity.  What is not seen has no effect, whatever it holds (NaN too).
+ * Scores, statistics and sums are float32; bf16 probabilities enter their product as one bf16 term (many rows per
+ * KV head) or two.  n_heads / n_kv_heads is an integer from 1 to 64; scale is positive. */
+typedef struct {
+    int32_t n_heads, dtype, window, sinks;
+    float scale;
+} ead_paged_attn;
+/* Bytes of device memory an attention call needs (0 possible).  The caller clears them once, before the first
+ * call that gets them; every call leaves what the next one expects.  A workspace serves one stream at a time. */
+ead_status ead_paged_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch,
+                               const ead_paged_attn *attn, uint64_t *bytes);
+ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_batch *batch,
+                               const ead_paged_attn *attn, const ead_rows *q, const ead_rows *out, float *lse,
+                               void *workspace, uint64_t workspace_bytes, void *hip_stream);
 
 /* ---- bookkeeping ----------------------------------------------------------------- */
 ead_status ead_get_stats(ead_handle *h, ead_stats *out);

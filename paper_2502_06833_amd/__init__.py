@@ -6,3 +6,4 @@ There is no CPU fallback: loading fails loudly if the library has not been built
 """
 from .binding import (EAD, BITS, NATS, SMALL, LARGE, EadError, Gate, entropy_argmax, lib,  # noqa: F401
                       exported_symbols)
+from .paged import PagedBatch, PagedCache  # noqa: F401

@@ -87,6 +87,11 @@ _SIGNATURES = {
     "ead_set_fused": (C.c_int, [C.c_void_p, C.c_int32]),
     "ead_set_schedule": (C.c_int, [C.c_void_p, C.c_int32, C.c_float, C.c_float]),
     "ead_set_sampling": (C.c_int, [C.c_void_p, C.c_float, C.c_uint64]),
+    "ead_paged_write": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ead_paged_read": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ead_paged_workspace": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_uint64)]),
+    "ead_paged_attention": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_uint64, C.c_void_p]),
     "ead_profile_enable": (C.c_int, [C.c_void_p, C.c_int32]),
     "ead_profile_select": (C.c_int, [C.c_void_p, C.c_char_p]),
     "ead_profile_read": (C.c_int, [C.c_void_p, C.POINTER(KernelProfile), C.c_int32, _I32P]),

@@ -7,8 +7,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libead.so")
-SOURCES = ["ead.hip"]
-HEADERS = ["common.hpp", "linear.hpp", "attention.hpp", "entropy.hpp", "rules.hpp", "state.hpp", "fused.hpp", "stream_list.hpp", "stream.hpp", "turn.hpp"]
+SOURCES = ["ead.hip", "paged.hip"]
+HEADERS = ["common.hpp", "linear.hpp", "attention.hpp", "entropy.hpp", "rules.hpp", "state.hpp", "fused.hpp", "stream_list.hpp", "stream.hpp", "turn.hpp", "paged.hpp", "paged_rules.hpp"]
 
 
 def _newest_source() -> float:
@@ -25,7 +25,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     """hipcc cross-compiles for gfx950; no GPU is needed to build."""
     if not force and not is_stale():
         return LIB
-    cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-parallel-jobs=4",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
     r = subprocess.run(cmd, capture_output=True, text=True)

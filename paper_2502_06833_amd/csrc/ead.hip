@@ -332,6 +332,13 @@ ead_status fail(ead_handle *h, ead_status st, const char *fmt, ...) {
     return st;
 }
 
+}  // namespace
+namespace ead {
+// ead_last_error(NULL)'s text, for the calls that have no handle
+ead_status report(ead_status st, const char *text) { return fail(nullptr, st, "%s", text); }
+}  // namespace ead
+namespace {
+
 // the scratch set and stream the launches that follow use
 void use_lane(ead_handle *h, int i) {
     if (!h->two_lanes) i = 0;

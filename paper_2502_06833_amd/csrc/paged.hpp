@@ -1,0 +1,671 @@
+// A paged K/V cache in the caller's memory: rows written to it (rounded to its type), read back from it, and
+// attention of rows over it.
+//
+// Pages are [page][KV head][slot][head_dim]: what one head holds of a page is contiguous, so a wave that takes 16 keys
+// of a head reads (or writes) 16 * head_dim elements in a row, whatever the page size.
+#pragma once
+#include <type_traits>
+
+#include "common.hpp"
+
+namespace ead {
+
+struct fp8_t { uint8_t u; };      // an e4m3 code
+
+struct PagedArgs {
+    const void *k, *v;
+    const uint8_t *ks, *vs;                       // exponents of an 8-bit cache
+    int n_pages, page_shift, n_kv;
+    const int *table, *q_starts, *kv_lens;
+    int table_stride, table_width, rows;
+};
+
+// A sequence as the device arrays have it, cut to what the host vouched for: row0 + n_rows <= rows, 0 <= kv <= table.
+struct PagedSeq {
+    int row0, n_rows, kv, first;                  // first: position of its first row (below 0 where kv < n_rows)
+    const int *table;
+};
+__device__ __forceinline__ PagedSeq paged_seq(const PagedArgs &a, int b) {
+    PagedSeq s;
+    s.row0 = min(max(a.q_starts[b], 0), a.rows);
+    s.n_rows = min(max(a.q_starts[b + 1], s.row0), a.rows) - s.row0;
+    s.kv = min(max(a.kv_lens[b], 0), (int)min((long)a.table_width << a.page_shift, (long)0x7FFFFF00));
+    s.first = s.kv - s.n_rows;
+    s.table = a.table + (size_t)b * a.table_stride;
+    return s;
+}
+// The page of a position 0 <= pos < kv; -1: a hole
+__device__ __forceinline__ int paged_page(const PagedArgs &a, const PagedSeq &s, int pos) {
+    const int id = s.table[pos >> a.page_shift];
+    return (unsigned)id < (unsigned)a.n_pages ? id : -1;
+}
+// Vector (page, head, slot)'s number in the pool: 64 bits, since a pool may hold more than 2^31 elements
+__device__ __forceinline__ size_t paged_vec(const PagedArgs &a, int page, int h, int slot) {
+    return (((size_t)page * a.n_kv + h) << a.page_shift) + slot;
+}
+
+// ---- 8 bits: e4m3 codes times a power of two per vector --------------------------------------
+// e4m3 reaches from 2^-9 to 448 with three fraction bits; a power-of-two scale moves that range over the vector and
+// costs no fraction bit, so the scale is a byte and codes times scale are exact in bf16 (8 fraction bits).
+__device__ __forceinline__ int fp8_exponent(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    const int e = (int)(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u);     // 448 = 1.75 * 2^8
+    return min(max(e, 1), 254);
+}
+__device__ __forceinline__ float exp2_of(int biased) { return __uint_as_float((uint32_t)biased << 23); }
+__device__ __forceinline__ uint32_t fp8_pack4(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+// two codes of a word (its low or high half) times a power of two, as a pair of bf16
+template <bool HIGH>
+__device__ __forceinline__ uint32_t fp8_bf16x2(uint32_t w, float scale) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, (bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HIGH));
+}
+
+// ---- write and read ----------------------------------------------------------------------------
+struct RowsArg {
+    const void *p;
+    long row_stride, head_stride;
+    int vec;                        // every vector starts on a 16-byte boundary
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int vec, float (&f)[8]) {
+    if (vec) {
+        Vec8<T> x;
+        x.load(p);
+        x.unpack(f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = to_f32(p[e]);
+    }
+}
+// eight floats as bf16, NaN kept (the conversion instruction)
+__device__ __forceinline__ u32x4_t bf16x8_of(const float (&f)[8]) {
+    return u32x4_t{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+}
+
+// One vector's eight elements of this lane to the cache.  The HD / 8 lanes that share a vector call it together.
+template <typename CT, int HD>
+__device__ __forceinline__ void put8(void *pool, uint8_t *scales, size_t vec, int lane, float (&f)[8], bool live) {
+    if constexpr (sizeof(CT) == 1) {
+        float m = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float a = __builtin_fabsf(f[e]);
+            m = a <= 3.402823466e38f ? fmaxf(m, a) : m;
+        }
+#pragma unroll
+        for (int o = HD / 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+        const int ex = fp8_exponent(m);
+        const float inv = exp2_of(254 - ex);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = __builtin_fabsf(f[e]) <= 3.402823466e38f ? f[e] * inv : __builtin_nanf("");
+        if (live) {
+            uint2 w;
+            w.x = fp8_pack4(f[0], f[1], f[2], f[3]);
+            w.y = fp8_pack4(f[4], f[5], f[6], f[7]);
+            *(uint2 *)((uint8_t *)pool + vec * HD + lane * 8) = w;
+            if (lane == 0) scales[vec] = (uint8_t)ex;
+        }
+    } else if constexpr (sizeof(CT) == 2) {
+        if (live) *(u32x4_t *)((bf16_t *)pool + vec * HD + lane * 8) = bf16x8_of(f);
+    } else {
+        if (live) store8<float>((float *)pool + vec * HD + lane * 8, f);
+    }
+}
+
+// The rows' vectors are taken in the order [block of 2^tb tokens][head][token]: with many rows a workgroup writes runs
+// of neighbouring slots, with one row per sequence (tb = 0) it takes the heads of that row.
+struct PagedCopy {
+    PagedArgs a;
+    RowsArg k, v;
+    int tb;
+};
+struct PagedItem { int t, h; };
+__device__ __forceinline__ PagedItem paged_item(const PagedCopy &c, int i) {
+    const int hb = i >> c.tb;
+    return {(hb / c.a.n_kv << c.tb) | (i & ((1 << c.tb) - 1)), hb % c.a.n_kv};
+}
+
+template <typename CT, typename RT, int HD>
+__global__ __launch_bounds__(256) void k_paged_write(PagedCopy c) {
+    constexpr int L = HD / 8, kVecs = 256 / L;
+    const PagedSeq s = paged_seq(c.a, blockIdx.y);
+    const int total = ((s.n_rows + (1 << c.tb) - 1) >> c.tb << c.tb) * c.a.n_kv;
+    const int lane = (int)threadIdx.x % L;
+    for (int i = (int)blockIdx.x * kVecs + (int)threadIdx.x / L; i < total; i += (int)gridDim.x * kVecs) {
+        const PagedItem it = paged_item(c, i);
+        const int pos = s.first + it.t;
+        bool live = it.t < s.n_rows && pos >= 0;
+        float fk[8] = {}, fv[8] = {};
+        size_t vec = 0;
+        if (live) {
+            const size_t row = (size_t)(s.row0 + it.t);
+            load8((const RT *)c.k.p + row * c.k.row_stride + it.h * c.k.head_stride + lane * 8, c.k.vec, fk);
+            load8((const RT *)c.v.p + row * c.v.row_stride + it.h * c.v.head_stride + lane * 8, c.v.vec, fv);
+            const int page = paged_page(c.a, s, pos);
+            live = page >= 0;
+            vec = paged_vec(c.a, max(page, 0), it.h, pos & ((1 << c.a.page_shift) - 1));
+        }
+        put8<CT, HD>((void *)c.a.k, (uint8_t *)c.a.ks, vec, lane, fk, live);
+        put8<CT, HD>((void *)c.a.v, (uint8_t *)c.a.vs, vec, lane, fv, live);
+    }
+}
+
+template <typename CT, int HD>
+__device__ __forceinline__ void get8(const void *pool, const uint8_t *scales, size_t vec, int lane, float (&f)[8]) {
+    if constexpr (sizeof(CT) == 1) {
+        typedef float f32x2_t __attribute__((ext_vector_type(2)));
+        const uint2 w = *(const uint2 *)((const uint8_t *)pool + vec * HD + lane * 8);
+        const float scale = exp2_of(scales[vec]);
+        const f32x2_t p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w.x, false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w.x, true);
+        const f32x2_t p2 = __builtin_amdgcn_cvt_pk_f32_fp8(w.y, false), p3 = __builtin_amdgcn_cvt_pk_f32_fp8(w.y, true);
+        f[0] = p0.x * scale; f[1] = p0.y * scale; f[2] = p1.x * scale; f[3] = p1.y * scale;
+        f[4] = p2.x * scale; f[5] = p2.y * scale; f[6] = p3.x * scale; f[7] = p3.y * scale;
+    } else {
+        load8((const CT *)pool + vec * HD + lane * 8, 1, f);
+    }
+}
+template <typename RT>
+__device__ __forceinline__ void set8(RT *p, int vec, const float (&f)[8]) {
+    if (vec) {
+        if constexpr (sizeof(RT) == 2) *(u32x4_t *)p = bf16x8_of(f);
+        else store8<float>(p, f);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (sizeof(RT) == 2) p[e].u = (uint16_t)pack_bf16(f[e], 0.f);
+        else p[e] = f[e];
+    }
+}
+
+template <typename CT, typename RT, int HD>
+__global__ __launch_bounds__(256) void k_paged_read(PagedCopy c) {
+    constexpr int L = HD / 8, kVecs = 256 / L;
+    const PagedSeq s = paged_seq(c.a, blockIdx.y);
+    const int total = ((s.n_rows + (1 << c.tb) - 1) >> c.tb << c.tb) * c.a.n_kv;
+    const int lane = (int)threadIdx.x % L;
+    for (int i = (int)blockIdx.x * kVecs + (int)threadIdx.x / L; i < total; i += (int)gridDim.x * kVecs) {
+        const PagedItem it = paged_item(c, i);
+        if (it.t >= s.n_rows) continue;
+        const int pos = s.first + it.t;
+        const int page = pos >= 0 ? paged_page(c.a, s, pos) : -1;
+        float fk[8] = {}, fv[8] = {};
+        if (page >= 0) {
+            const size_t vec = paged_vec(c.a, page, it.h, pos & ((1 << c.a.page_shift) - 1));
+            get8<CT, HD>(c.a.k, c.a.ks, vec, lane, fk);
+            get8<CT, HD>(c.a.v, c.a.vs, vec, lane, fv);
+        }
+        const size_t row = (size_t)(s.row0 + it.t);
+        set8((RT *)c.k.p + row * c.k.row_stride + it.h * c.k.head_stride + lane * 8, c.k.vec, fk);
+        set8((RT *)c.v.p + row * c.v.row_stride + it.h * c.v.head_stride + lane * 8, c.v.vec, fv);
+    }
+}
+
+// ---- attention -----------------------------------------------------------------------------------
+struct PagedAttn {
+    PagedArgs a;
+    RowsArg q, out;
+    float *lse;
+    int n_heads, group;             // group: query heads per KV head
+    float c2;                       // scale * log2(e): scores are kept in units of one bit
+    int window, sinks;
+    int row_tiles, splits, split_tiles;   // grid.x = row_tiles * splits * n_kv; at least split_tiles key tiles to a split
+    float *part_o;                  // [unit][split][tile row][head_dim], relative to the split's maximum
+    float2 *part_ml;                // [unit][split][tile row]: maximum (in bits), sum
+    int *tickets;                   // [unit], zero between launches
+};
+
+constexpr int kKeyTile = 32;
+
+// What a tile of rows sees.  Rows of a KV head are (token, head of the group) pairs, token first: row = token * group + head.
+struct PagedTile {
+    int r0, rows;                   // first row, rows in the tile (0: none)
+    int p_lo, p_hi;                 // positions of its first and last row
+    int n_sink, t_lo, tiles;        // key tiles: n_sink ones from position 0, the others from tile t_lo on
+};
+__device__ __forceinline__ PagedTile paged_tile(const PagedAttn &c, const PagedSeq &s, int tile, int tile_rows) {
+    PagedTile t;
+    t.r0 = tile * tile_rows;
+    t.rows = min(max(s.n_rows * c.group - t.r0, 0), tile_rows);
+    t.p_lo = s.first + t.r0 / c.group;
+    t.p_hi = s.first + (t.r0 + max(t.rows, 1) - 1) / c.group;
+    t.t_lo = c.window ? max(0, t.p_lo - c.window + 1) / kKeyTile : 0;
+    t.n_sink = c.window ? min((min(c.sinks, s.kv) + kKeyTile - 1) / kKeyTile, t.t_lo) : 0;
+    t.tiles = t.rows > 0 && t.p_hi >= 0 ? t.n_sink + max(t.p_hi / kKeyTile + 1 - t.t_lo, 0) : 0;
+    return t;
+}
+__device__ __forceinline__ bool paged_sees(const PagedAttn &c, int pos, int key) {
+    return key <= pos && (!c.window || pos - key < c.window || key < c.sinks);
+}
+
+// N bytes of device memory as words; N = 2: the half word in the low bits
+template <int N> struct Raw {
+    static constexpr int kWords = N < 4 ? 1 : N / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const void *p) {
+        if constexpr (N == 2) w[0] = *(gptr<uint16_t>)p;
+        else if constexpr (N == 4) w[0] = *(gptr<uint32_t>)p;
+        else if constexpr (N == 8) { typedef uint32_t u32x2_t __attribute__((ext_vector_type(2))); const u32x2_t x = *(gptr<u32x2_t>)p; w[0] = x.x; w[1] = x.y; }
+        else {
+#pragma unroll
+            for (int i = 0; i < N / 16; ++i) {
+                const u32x4_t x = ((gptr<u32x4_t>)p)[i];
+                w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+            }
+        }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0u;
+    }
+};
+
+// One wave's piece of attention: a tile of 32 keys against NB blocks of 16 rows, everything in registers.
+//
+//  S^T = K Q^T: the keys are the M of the product, rows the N, so lane (n, g) = (lane & 15, lane >> 4) gets the scores of row n
+//  for keys 4g .. 4g+3 of each half of the tile: statistics are the lane's own up to two shuffles over g, and the lane
+//  already holds what the second product, O^T = V^T P^T, wants of P: its contraction runs over the keys in the order
+//  (j < 4 ? 4g + j : 16 + 4g + j - 4), in which V's rows are loaded.  V's M order is free too: lane n loads VW = HD/16
+//  neighbouring elements of each of its eight keys, the products c = 0 .. VW-1 take element c of every lane, and a
+//  lane ends up with the HD/4 neighbouring output elements VW (4g + r) + c of row n.  Turning eight
+//  keys x VW elements into VW operands is one byte permute per word; nothing goes through LDS.
+template <typename CT, int HD, int NB>
+struct PagedWave {
+    static constexpr bool F32 = sizeof(CT) == 4, F8 = sizeof(CT) == 1;
+    static constexpr int VW = F32 ? (HD / 16 < 4 ? HD / 16 : 4) : HD / 16;   // neighbouring elements of V in one load
+    static constexpr int VC = HD / 16 / VW;                                  // loads per key (2 for float, HD 128)
+    // K's contraction order is free as long as Q's is the same: a lane takes KE neighbouring elements at a time
+    static constexpr int KE = F32 ? 4 : F8 ? (HD >= 64 ? 16 : 8) : 8;
+    static constexpr int KL = HD / 4 / KE;                                   // loads per key
+    static constexpr int QW = F32 ? HD / 4 : HD / 8;                         // words of Q per lane
+
+    // a second tile's words fit beside the queries, the outputs and the scores
+    static constexpr bool kAhead = 2 * (HD / 2) * (int)sizeof(CT) / 2 + NB * (QW + HD / 4 + 16) <= 264;
+
+    uint32_t q[NB][QW];
+    f32x4_t o[NB][HD / 16];
+    float m[NB], l[NB];             // in bits; l: this lane's keys only
+
+    struct Keys {                   // what a wave has requested of a tile
+        Raw<KE * (int)sizeof(CT)> k[2][KL];
+        Raw<VW * (int)sizeof(CT)> v[8][VC];
+        uint32_t ks[2], vs[2];      // exponents: K of key n of each half; V of keys 4g..4g+3 of each half
+        int base;                   // first position
+        int page[2];                // of each half; -1: a hole or past the end
+    };
+
+    __device__ __forceinline__ void init(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int lane) {
+        const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int row = b * 16 + n;
+            m[b] = -INFINITY;
+            l[b] = 0.f;
+#pragma unroll
+            for (int i = 0; i < HD / 16; ++i) o[b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < QW; ++i) q[b][i] = 0u;
+            if (row < t.rows) {
+                const int r = t.r0 + row, tok = r / c.group, qh = h * c.group + r % c.group;
+                const size_t at = (size_t)(s.row0 + tok) * c.q.row_stride + (size_t)qh * c.q.head_stride;
+#pragma unroll
+                for (int i = 0; i < KL; ++i) {
+                    const int d = i * 4 * KE + g * KE;
+                    if constexpr (F32) {
+                        const float *p = (const float *)c.q.p + at + d;
+                        if (c.q.vec) { Raw<16> x; x.load(p); for (int e = 0; e < 4; ++e) q[b][i * 4 + e] = x.w[e]; }
+                        else for (int e = 0; e < 4; ++e) q[b][i * 4 + e] = __float_as_uint(p[e]);
+                    } else {
+                        const bf16_t *p = (const bf16_t *)c.q.p + at + d;
+                        if (c.q.vec) { Raw<KE * 2> x; x.load(p); for (int e = 0; e < KE / 2; ++e) q[b][i * (KE / 2) + e] = x.w[e]; }
+                        else for (int e = 0; e < KE / 2; ++e) q[b][i * (KE / 2) + e] = (uint32_t)p[2 * e].u | (uint32_t)p[2 * e + 1].u << 16;
+                    }
+                }
+            }
+        }
+    }
+
+    // Every address is inside the pool: halves without a page (holes, positions past the end) read page 0 and are masked
+    __device__ __forceinline__ void load(const PagedAttn &c, const PagedSeq &s, int tile, int h, int lane, Keys &x) const {
+        const int n = lane & 15, g = lane >> 4;
+        x.base = tile * kKeyTile;
+        const int mask = (1 << c.a.page_shift) - 1;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int pos = x.base + 16 * half;
+            x.page[half] = pos < s.kv ? paged_page(c.a, s, pos) : -1;
+            const size_t vec = paged_vec(c.a, max(x.page[half], 0), h, pos & mask);
+            const CT *k = (const CT *)c.a.k + vec * HD, *v = (const CT *)c.a.v + vec * HD;
+#pragma unroll
+            for (int i = 0; i < KL; ++i) x.k[half][i].load(k + n * HD + i * 4 * KE + g * KE);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < VC; ++i) x.v[half * 4 + j][i].load(v + (4 * g + j) * HD + i * 16 * VW + n * VW);
+            if constexpr (F8) {
+                x.ks[half] = *(gptr<uint8_t>)(c.a.ks + vec + n);
+                x.vs[half] = *(gptr<uint32_t>)(c.a.vs + vec + 4 * g);
+            }
+        }
+    }
+
+    __device__ __forceinline__ static int key_of(int base, int j, int g) { return base + (j < 4 ? 4 * g + j : 12 + 4 * g + j); }
+
+    __device__ __forceinline__ void take(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int lane, Keys &x) {
+        const int n = lane & 15, g = lane >> 4;
+        // ---- scores
+        f32x4_t sc[NB][2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sc[b][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KL; ++i) {
+                if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+                            sc[b][half] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.k[half][i].w[e]), __uint_as_float(q[b][i * 4 + e]), sc[b][half], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < KE / 8; ++e) {
+                        u32x4_t kw;
+                        if constexpr (F8) {
+                            const float ks = exp2_of((int)x.ks[half]);
+                            kw = u32x4_t{fp8_bf16x2<false>(x.k[half][i].w[2 * e], ks), fp8_bf16x2<true>(x.k[half][i].w[2 * e], ks),
+                                         fp8_bf16x2<false>(x.k[half][i].w[2 * e + 1], ks), fp8_bf16x2<true>(x.k[half][i].w[2 * e + 1], ks)};
+                        } else {
+                            kw = u32x4_t{x.k[half][i].w[0], x.k[half][i].w[1], x.k[half][i].w[2], x.k[half][i].w[3]};
+                        }
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) {
+                            const int w = i * (KE / 2) + e * 4;
+                            const u32x4_t qw = {q[b][w], q[b][w + 1], q[b][w + 2], q[b][w + 3]};
+                            sc[b][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kw), __builtin_bit_cast(bf16x8_t, qw), sc[b][half], 0, 0, 0);
+                        }
+                    }
+                }
+            }
+        }
+        // ---- masks: a tile that every row sees whole has none
+        const int last = x.base + kKeyTile - 1;
+        const bool whole = x.page[0] >= 0 && x.page[1] >= 0 && last <= t.p_lo && (!c.window || t.p_hi - x.base < c.window || last < c.sinks);
+        if (!whole) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int pos = s.first + (t.r0 + b * 16 + n) / c.group;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool sees = x.page[j >> 2] >= 0 && paged_sees(c, pos, key_of(x.base, j, g));
+                    sc[b][j >> 2][j & 3] = sees ? sc[b][j >> 2][j & 3] : -INFINITY;
+                }
+            }
+            // V of keys that hold nothing any row sees: whatever lies there, 0 times it has to be 0
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int key = key_of(x.base, j, g);
+                const bool any = x.page[j >> 2] >= 0 && key <= t.p_hi && (!c.window || t.p_lo - key < c.window || key < c.sinks);
+                if (!any) {
+#pragma unroll
+                    for (int i = 0; i < VC; ++i) x.v[j][i].zero();
+                }
+            }
+        }
+        // ---- running maximum and sum.  The maximum that the sums refer to follows the true one only when that is more
+        // than 8 bits above it: exponentials stay below 2^8, and the output is seldom rescaled.
+        float p[NB][8];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, sc[b][j >> 2][j & 3]);
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave)) * c.c2;
+            if (__any(top > m[b] + 8.f)) {
+                const float to = fmaxf(m[b], top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[b] - to);
+                m[b] = to;
+                l[b] *= f;
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[b][i][r] *= f;
+            }
+            const float ref = m[b] == -INFINITY ? 0.f : m[b];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                p[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][j >> 2][j & 3], c.c2, -ref));
+                l[b] += p[b][j];
+            }
+        }
+        // ---- output
+        if constexpr (F32) {
+            bool odd = false;
+            if (!whole) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int i = 0; i < VC; ++i)
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) {
+                            const bool bad = (x.v[j][i].w[e] & 0x7F800000u) == 0x7F800000u;
+                            odd |= bad;
+                            x.v[j][i].w[e] = bad ? 0u : x.v[j][i].w[e];
+                        }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < VC; ++i)
+#pragma unroll
+                    for (int e = 0; e < VW; ++e)
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+                            o[b][i * VW + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[j][i].w[e]), p[b][j], o[b][i * VW + e], 0, 0, 0);
+            if (__any(odd)) add_odd(c, s, t, h, lane, x);
+        } else {
+            // two bf16 terms of every probability
+            u32x4_t hi[NB], lo[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                hi[b] = __builtin_bit_cast(u32x4_t, take_bf16(p[b]));
+                lo[b] = u32x4_t{pack_bf16(p[b][0], p[b][1]), pack_bf16(p[b][2], p[b][3]), pack_bf16(p[b][4], p[b][5]), pack_bf16(p[b][6], p[b][7])};
+            }
+            bool odd = false;
+#pragma unroll
+            for (int d = 0; d < VW / 2; ++d) {
+                uint32_t w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (F8) {
+                        const float vs = exp2_of((int)((x.vs[j >> 2] >> (8 * (j & 3))) & 0xFFu));
+                        const uint32_t word = x.v[j][0].w[d >> 1];
+                        w[j] = (d & 1) ? fp8_bf16x2<true>(word, vs) : fp8_bf16x2<false>(word, vs);
+                    } else {
+                        w[j] = x.v[j][0].w[d];
+                    }
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool b0 = (w[j] & 0x7F80u) == 0x7F80u, b1 = (w[j] & 0x7F800000u) == 0x7F800000u;
+                        odd |= b0 || b1;
+                        w[j] &= (b0 ? 0xFFFF0000u : 0xFFFFFFFFu) & (b1 ? 0xFFFFu : 0xFFFFFFFFu);
+                    }
+                }
+                u32x4_t va, vb;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    va[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
+                    vb[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    o[b][2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, hi[b]), o[b][2 * d], 0, 0, 0);
+                    o[b][2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vb), __builtin_bit_cast(bf16x8_t, hi[b]), o[b][2 * d + 1], 0, 0, 0);
+                    o[b][2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, lo[b]), o[b][2 * d], 0, 0, 0);
+                    o[b][2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vb), __builtin_bit_cast(bf16x8_t, lo[b]), o[b][2 * d + 1], 0, 0, 0);
+                }
+            }
+            if (__any(odd)) add_odd(c, s, t, h, lane, x);
+        }
+    }
+
+    // Output element i (0 .. HD/16-1), r of this lane is dimension dim_of(i, r, g) of its row
+    __device__ __forceinline__ static int dim_of(int i, int r, int g) { return (i / VW) * 16 * VW + VW * (4 * g + r) + i % VW; }
+
+    // Infinities and NaN among the values of a tile that some rows see and others do not: they were left out of the
+    // product, where a row that does not see them would have got 0 * NaN, and are added to the rows that do.
+    __device__ __forceinline__ void add_odd(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int lane, const Keys &x) {
+        const int n = lane & 15, g = lane >> 4;
+        for (int k = 0; k < kKeyTile; ++k) {
+            const int key = x.base + k, page = k < 16 ? x.page[0] : x.page[1];
+            if (page < 0 || key > t.p_hi) continue;
+            const size_t vec = paged_vec(c.a, page, h, key & ((1 << c.a.page_shift) - 1));
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int row = b * 16 + n, pos = s.first + (t.r0 + row) / c.group;
+                if (row >= t.rows || !paged_sees(c, pos, key)) continue;
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float v;
+                        if constexpr (F8) v = (((const uint8_t *)c.a.v)[vec * HD + dim_of(i, r, g)] & 0x7F) == 0x7F ? __builtin_nanf("") : 0.f;
+                        else v = to_f32(((const CT *)c.a.v)[vec * HD + dim_of(i, r, g)]);
+                        o[b][i][r] += __builtin_fabsf(v) <= 3.402823466e38f ? 0.f : v;
+                    }
+            }
+        }
+    }
+};
+
+template <typename T> __device__ __forceinline__ void put_out(const PagedAttn &c, size_t at, float v);
+template <> __device__ __forceinline__ void put_out<float>(const PagedAttn &c, size_t at, float v) { ((float *)c.out.p)[at] = v; }
+template <> __device__ __forceinline__ void put_out<bf16_t>(const PagedAttn &c, size_t at, float v) { ((bf16_t *)c.out.p)[at].u = (uint16_t)pack_bf16(v, 0.f); }
+
+// Attention of few rows per KV head, and of float32 models' rows however many: a workgroup takes NB blocks of 16 rows of one
+// KV head and a range of keys, its four waves every fourth tile of the range.  K and V go from memory to
+// registers and into the matrix cores; a wave requests a tile while it works on the one before.  The waves' results
+// are joined through LDS, the ranges' by the workgroup that arrives last.
+template <typename CT, int HD, int NB>
+__global__ __launch_bounds__(256) void k_paged_attn(PagedAttn c) {
+    using W = PagedWave<CT, HD, NB>;
+    using OT = typename std::conditional<sizeof(CT) == 4, float, bf16_t>::type;
+    __shared__ float ob[4][16][HD + 4];
+    __shared__ float2 ml[4][NB * 16];
+    __shared__ int last_one;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int h = (int)blockIdx.x % c.a.n_kv, rest = (int)blockIdx.x / c.a.n_kv;
+    const int split = rest % c.splits, tile = c.row_tiles - 1 - rest / c.splits;    // later rows see more: they start first
+    const PagedSeq s = paged_seq(c.a, blockIdx.y);
+    const PagedTile t = paged_tile(c, s, tile, NB * 16);
+    if (t.rows == 0) return;
+    const int per = max(c.split_tiles, (t.tiles + c.splits - 1) / c.splits), used = max(1, (t.tiles + per - 1) / per);
+    if (split >= used) return;
+    const int begin = split * per, end = min(begin + per, t.tiles);
+
+    W w;
+    w.init(c, s, t, h, lane);
+    auto key_tile = [&](int i) { return i < t.n_sink ? i : i - t.n_sink + t.t_lo; };
+    {
+        typename W::Keys x;
+        int i = begin + wave;
+        if constexpr (W::kAhead) {
+            typename W::Keys y;
+            if (i < end) w.load(c, s, key_tile(i), h, lane, x);
+            while (i < end) {
+                if (i + 4 < end) w.load(c, s, key_tile(i + 4), h, lane, y);
+                w.take(c, s, t, h, lane, x);
+                i += 4;
+                if (i >= end) break;
+                if (i + 4 < end) w.load(c, s, key_tile(i + 4), h, lane, x);
+                w.take(c, s, t, h, lane, y);
+                i += 4;
+            }
+        } else {
+            for (; i < end; i += 4) {
+                w.load(c, s, key_tile(i), h, lane, x);
+                w.take(c, s, t, h, lane, x);
+            }
+        }
+    }
+
+    const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        w.l[b] += __shfl_xor(w.l[b], 16, kWave);
+        w.l[b] += __shfl_xor(w.l[b], 32, kWave);
+        if (w.l[b] != w.l[b] && w.m[b] == -INFINITY) w.m[b] = 0.f;      // nothing but NaN: a NaN, not an empty row
+        if (g == 0) ml[wave][b * 16 + n] = make_float2(w.m[b], w.l[b]);
+    }
+    __syncthreads();
+    const size_t unit = ((size_t)blockIdx.y * c.a.n_kv + h) * c.row_tiles + tile;
+    auto finish = [&](int row, int d, float M, float L, float v) {
+        const int r = t.r0 + row, tok = r / c.group, qh = h * c.group + r % c.group;
+        const size_t at = (size_t)(s.row0 + tok) * c.out.row_stride + (size_t)qh * c.out.head_stride + d;
+        put_out<OT>(c, at, L == 0.f ? 0.f : v / L);
+        if (c.lse && d == 0) c.lse[(size_t)(s.row0 + tok) * c.n_heads + qh] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994531f;
+    };
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        float M = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) M = fmaxf(M, ml[i][b * 16 + n].x);
+        const float f = w.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m[b] - M);
+        if (b) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ob[wave][n][W::dim_of(i, r, g)] = w.m[b] == -INFINITY ? 0.f : w.o[b][i][r] * f;
+        __syncthreads();
+        const int row = (int)threadIdx.x >> 4;
+        if (b * 16 + row < t.rows) {
+            float R = -INFINITY, L = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) R = fmaxf(R, ml[i][b * 16 + row].x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { const float2 e = ml[i][b * 16 + row]; L += e.x == -INFINITY ? 0.f : e.y * __builtin_amdgcn_exp2f(e.x - R); }
+#pragma unroll
+            for (int i = 0; i < HD / 16; ++i) {
+                const int d = i * 16 + ((int)threadIdx.x & 15);
+                const float v = ob[0][row][d] + ob[1][row][d] + ob[2][row][d] + ob[3][row][d];
+                if (used == 1) finish(b * 16 + row, d, R, L, v);
+                else st_coherent(c.part_o + ((unit * c.splits + split) * (NB * 16) + b * 16 + row) * HD + d, v);
+            }
+            if (used > 1 && ((int)threadIdx.x & 15) == 0) {
+                float *p = (float *)(c.part_ml + (unit * c.splits + split) * (NB * 16) + b * 16 + row);
+                st_coherent(p, R);
+                st_coherent(p + 1, L);
+            }
+        }
+    }
+    if (used == 1) return;
+    wait_stores();
+    __syncthreads();
+    if (threadIdx.x == 0) last_one = __hip_atomic_fetch_add(c.tickets + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1;
+    __syncthreads();
+    if (!last_one) return;
+    if (threadIdx.x == 0) st_coherent(c.tickets + unit, 0);
+    for (int e = (int)threadIdx.x; e < t.rows * HD; e += 256) {
+        const int row = e / HD, d = e % HD;
+        const float *po = c.part_o + (unit * c.splits * (NB * 16) + row) * HD + d;
+        const float *pm = (const float *)(c.part_ml + unit * c.splits * (NB * 16) + row);
+        float M = -INFINITY, L = 0.f, v = 0.f;
+        for (int i = 0; i < used; ++i) M = fmaxf(M, ld_coherent(pm + (size_t)i * (NB * 16) * 2));
+        if (M != -INFINITY)
+            for (int i = 0; i < used; ++i) {
+                const float f = __builtin_amdgcn_exp2f(ld_coherent(pm + (size_t)i * (NB * 16) * 2) - M);
+                L += f * ld_coherent(pm + (size_t)i * (NB * 16) * 2 + 1);
+                v += f * ld_coherent(po + (size_t)i * (NB * 16) * HD);
+            }
+        finish(row, d, M, L, v);
+    }
+}
+
+}  // namespace ead
