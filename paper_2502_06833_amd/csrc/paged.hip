@@ -9,6 +9,7 @@
 #include <algorithm>
 
 #include "paged.hpp"
+#include "paged_chunk.hpp"
 #include "paged_rules.hpp"
 
 namespace ead { ead_status report(ead_status st, const char *text); }
@@ -136,10 +137,34 @@ ead_status check_attention(const ead_paged_cache *cache, const ead_paged_batch *
     return EAD_OK;
 }
 
-PagedPlan plan_of(const ead_paged_cache *cache, const ead_paged_batch *b, const ead_paged_attn *at) {
-    const long held = std::min((long)b->max_kv, (long)b->table_width * cache->page_size);
-    return paged_plan(b->batch, cache->n_kv_heads, at->n_heads / cache->n_kv_heads, b->max_q, (int)held, at->window, at->sinks, compute_units(),
-                      paged_max_blocks(cache->dtype == EAD_F32, cache->head_dim));
+// The launches of a call: sequences with few rows (of a float32 cache: all), then those with many
+struct PagedCall {
+    bool few, many, two;
+    PagedPlan f, m;
+    uint64_t f_bytes, m_bytes;
+};
+PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_paged_attn *at) {
+    const int held = (int)std::min((long)b->max_kv, (long)b->table_width * c->page_size), group = at->n_heads / c->n_kv_heads, cus = compute_units();
+    const bool f32 = c->dtype == EAD_F32;
+    const long rows = (long)b->max_q * group;
+    PagedCall p{};
+    p.few = f32 || (long)b->min_q * group <= kPagedFewRows;
+    p.many = !f32 && rows > kPagedFewRows;
+    if (p.few) p.f = paged_few(b->batch, c->n_kv_heads, group, f32 ? rows : std::min(rows, (long)kPagedFewRows), held, at->window, at->sinks, cus, paged_max_blocks(f32, c->head_dim));
+    if (p.many) p.m = paged_many(b->batch, c->n_kv_heads, group, rows, held, at->window, at->sinks, cus);
+    p.two = paged_keys(128, 64, group, held, at->window, at->sinks) <= kPagedTwoTerms;
+    p.f_bytes = p.few ? paged_bytes(p.f, c->head_dim) : 0;
+    p.m_bytes = p.many ? paged_bytes(p.m, c->head_dim) : 0;
+    return p;
+}
+
+// the plan and its part of the workspace
+dim3 set_plan(PagedAttn &c, const PagedPlan &p, char *ws, int batch) {
+    c.row_tiles = p.row_tiles; c.splits = p.splits; c.split_tiles = p.split_tiles;
+    c.tickets = (int *)ws;
+    c.part_ml = (float2 *)(ws + (p.units + 63) / 64 * 256);
+    c.part_o = (float *)(c.part_ml + (size_t)p.units * p.splits * p.tile_rows);
+    return dim3((unsigned)((long)p.row_tiles * p.splits * c.a.n_kv), (unsigned)batch);
 }
 
 }  // namespace
@@ -160,7 +185,8 @@ ead_status ead_paged_workspace(const ead_paged_cache *cache, const ead_paged_bat
     if (!bytes) return refuse(EAD_ERR_INVALID_ARG, "bytes is null");
     *bytes = 0;
     PAGED_TRY(check_attention(cache, batch, attn));
-    *bytes = paged_bytes(plan_of(cache, batch, attn), cache->head_dim);
+    const PagedCall p = plan_of(cache, batch, attn);
+    *bytes = p.f_bytes + p.m_bytes;
     return EAD_OK;
 }
 
@@ -171,8 +197,8 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     PagedAttn c{};
     PAGED_TRY(rows_of(q, attn->dtype, "q", &c.q));
     PAGED_TRY(rows_of(out, attn->dtype, "out", &c.out));
-    const PagedPlan p = plan_of(cache, batch, attn);
-    const uint64_t need = paged_bytes(p, cache->head_dim);
+    const PagedCall p = plan_of(cache, batch, attn);
+    const uint64_t need = p.f_bytes + p.m_bytes;
     if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
         return refuse(EAD_ERR_INVALID_ARG, "workspace: %llu bytes, 16-byte aligned, are needed", (unsigned long long)need);
     c.a = args_of(cache, batch);
@@ -182,20 +208,29 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     c.c2 = attn->scale * 1.4426950408889634f;
     c.window = attn->window;
     c.sinks = attn->sinks;
-    c.row_tiles = p.row_tiles; c.splits = p.splits; c.split_tiles = p.split_tiles;
-    if (need) {
-        c.tickets = (int *)workspace;
-        c.part_ml = (float2 *)((char *)workspace + (p.units + 63) / 64 * 256);
-        c.part_o = (float *)(c.part_ml + (size_t)p.units * p.splits * 16 * p.nb);
+    const bool f32 = cache->dtype == EAD_F32;
+    c.few_rows = f32 ? 0x7FFFFFFF : kPagedFewRows;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    if (p.few) {
+        const dim3 grid = set_plan(c, p.f, (char *)workspace, batch->batch);
+        with_cache(cache, [&](auto ct, auto hd) {
+            using CT = decltype(ct);
+            constexpr int HD = decltype(hd)::value;
+            if (p.f.tile_rows == 16) hipLaunchKernelGGL((k_paged_attn<CT, HD, 1>), grid, dim3(256), 0, st, c);
+            else if (p.f.tile_rows == 32) hipLaunchKernelGGL((k_paged_attn<CT, HD, 2>), grid, dim3(256), 0, st, c);
+            else if constexpr (paged_max_blocks(sizeof(CT) == 4, HD) == 4) hipLaunchKernelGGL((k_paged_attn<CT, HD, 4>), grid, dim3(256), 0, st, c);
+        });
     }
-    const dim3 grid((unsigned)((long)p.row_tiles * p.splits * cache->n_kv_heads), (unsigned)batch->batch);
-    with_cache(cache, [&](auto ct, auto hd) {
-        using CT = decltype(ct);
-        constexpr int HD = decltype(hd)::value;
-        if (p.nb == 1) hipLaunchKernelGGL((k_paged_attn<CT, HD, 1>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
-        else if (p.nb == 2) hipLaunchKernelGGL((k_paged_attn<CT, HD, 2>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
-        else if constexpr (paged_max_blocks(sizeof(CT) == 4, HD) == 4) hipLaunchKernelGGL((k_paged_attn<CT, HD, 4>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
-    });
+    if (p.many) {
+        const dim3 grid = set_plan(c, p.m, (char *)workspace + p.f_bytes, batch->batch);
+        with_cache(cache, [&](auto ct, auto hd) {
+            using CT = decltype(ct);
+            if constexpr (sizeof(CT) != 4) {
+                if (p.two) hipLaunchKernelGGL((k_paged_chunk<CT, decltype(hd)::value, true>), grid, dim3(256), 0, st, c);
+                else hipLaunchKernelGGL((k_paged_chunk<CT, decltype(hd)::value, false>), grid, dim3(256), 0, st, c);
+            }
+        });
+    }
     return launched("ead_paged_attention");
 }
 

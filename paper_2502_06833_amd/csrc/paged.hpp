@@ -214,6 +214,7 @@ struct PagedAttn {
     int n_heads, group;             // group: query heads per KV head
     float c2;                       // scale * log2(e): scores are kept in units of one bit
     int window, sinks;
+    int few_rows;                   // sequences with at most this many rows per KV head are k_paged_attn's, the others k_paged_chunk's
     int row_tiles, splits, split_tiles;   // grid.x = row_tiles * splits * n_kv; at least split_tiles key tiles to a split
     float *part_o;                  // [unit][split][tile row][head_dim], relative to the split's maximum
     float2 *part_ml;                // [unit][split][tile row]: maximum (in bits), sum
@@ -228,15 +229,16 @@ struct PagedTile {
     int p_lo, p_hi;                 // positions of its first and last row
     int n_sink, t_lo, tiles;        // key tiles: n_sink ones from position 0, the others from tile t_lo on
 };
+template <int KEYS>
 __device__ __forceinline__ PagedTile paged_tile(const PagedAttn &c, const PagedSeq &s, int tile, int tile_rows) {
     PagedTile t;
     t.r0 = tile * tile_rows;
     t.rows = min(max(s.n_rows * c.group - t.r0, 0), tile_rows);
     t.p_lo = s.first + t.r0 / c.group;
     t.p_hi = s.first + (t.r0 + max(t.rows, 1) - 1) / c.group;
-    t.t_lo = c.window ? max(0, t.p_lo - c.window + 1) / kKeyTile : 0;
-    t.n_sink = c.window ? min((min(c.sinks, s.kv) + kKeyTile - 1) / kKeyTile, t.t_lo) : 0;
-    t.tiles = t.rows > 0 && t.p_hi >= 0 ? t.n_sink + max(t.p_hi / kKeyTile + 1 - t.t_lo, 0) : 0;
+    t.t_lo = c.window ? max(0, t.p_lo - c.window + 1) / KEYS : 0;
+    t.n_sink = c.window ? min((min(c.sinks, s.kv) + KEYS - 1) / KEYS, t.t_lo) : 0;
+    t.tiles = t.rows > 0 && t.p_hi >= 0 ? t.n_sink + max(t.p_hi / KEYS + 1 - t.t_lo, 0) : 0;
     return t;
 }
 __device__ __forceinline__ bool paged_sees(const PagedAttn &c, int pos, int key) {
@@ -427,8 +429,8 @@ struct PagedWave {
             for (int j = 0; j < 8; ++j) top = fmaxf(top, sc[b][j >> 2][j & 3]);
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave)) * c.c2;
-            if (__any(top > m[b] + 8.f)) {
-                const float to = fmaxf(m[b], top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[b] - to);
+            if (__any(top > m[b] + 8.f)) {           // rows that need none keep theirs: what a row gets is its own affair
+                const float to = top > m[b] + 8.f ? top : m[b], f = top > m[b] + 8.f ? __builtin_amdgcn_exp2f(m[b] - to) : 1.f;
                 m[b] = to;
                 l[b] *= f;
 #pragma unroll
@@ -549,6 +551,51 @@ template <typename T> __device__ __forceinline__ void put_out(const PagedAttn &c
 template <> __device__ __forceinline__ void put_out<float>(const PagedAttn &c, size_t at, float v) { ((float *)c.out.p)[at] = v; }
 template <> __device__ __forceinline__ void put_out<bf16_t>(const PagedAttn &c, size_t at, float v) { ((bf16_t *)c.out.p)[at].u = (uint16_t)pack_bf16(v, 0.f); }
 
+// Output d of a tile's row from its maximum, sum and weighted values; with d = 0 its log-sum-exp
+template <typename OT>
+__device__ __forceinline__ void paged_finish(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int row, int d, float M, float L, float v) {
+    const int r = t.r0 + row, tok = r / c.group, qh = h * c.group + r % c.group;
+    put_out<OT>(c, (size_t)(s.row0 + tok) * c.out.row_stride + (size_t)qh * c.out.head_stride + d, L == 0.f ? 0.f : v / L);
+    if (c.lse && d == 0) c.lse[(size_t)(s.row0 + tok) * c.n_heads + qh] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994531f;
+}
+
+// Whether this workgroup is the last of a unit's `used` to have written its part (its stores were st_coherent); leaves the ticket at zero
+__device__ __forceinline__ bool paged_last(const PagedAttn &c, size_t unit, int used, int *shared) {
+    wait_stores();
+    __syncthreads();
+    if (threadIdx.x == 0) *shared = __hip_atomic_fetch_add(c.tickets + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1;
+    __syncthreads();
+    if (!*shared) return false;
+    if (threadIdx.x == 0) st_coherent(c.tickets + unit, 0);
+    // what the others wrote through is read from here on (each thread drops what it may hold of it)
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    return true;
+}
+
+// The parts of a unit joined: their order is that of the key ranges, whoever arrived last
+template <typename OT, int HD>
+__device__ __forceinline__ void paged_join(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, size_t unit, int used, int tile_rows) {
+    for (int e = (int)threadIdx.x; e < t.rows * (HD / 4); e += 256) {
+        const int row = e / (HD / 4), d = e % (HD / 4) * 4;
+        const float *po = c.part_o + (unit * c.splits * tile_rows + row) * HD + d;
+        const float2 *pm = c.part_ml + unit * c.splits * tile_rows + row;
+        float M = -INFINITY, L = 0.f;
+        f32x4e_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 16
+        for (int i = 0; i < used; ++i) M = fmaxf(M, pm[(size_t)i * tile_rows].x);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll 16
+        for (int i = 0; i < used; ++i) {
+            const float2 x = pm[(size_t)i * tile_rows];
+            const float f = __builtin_amdgcn_exp2f(x.x - ref);
+            L += f * x.y;
+            v += f * *(const f32x4e_t *)(po + (size_t)i * tile_rows * HD);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) paged_finish<OT>(c, s, t, h, row, d + i, M, L, v[i]);
+    }
+}
+
 // Attention of few rows per KV head, and of float32 models' rows however many: a workgroup takes NB blocks of 16 rows of one
 // KV head and a range of keys, its four waves every fourth tile of the range.  K and V go from memory to
 // registers and into the matrix cores; a wave requests a tile while it works on the one before.  The waves' results
@@ -564,7 +611,8 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedAttn c) {
     const int h = (int)blockIdx.x % c.a.n_kv, rest = (int)blockIdx.x / c.a.n_kv;
     const int split = rest % c.splits, tile = c.row_tiles - 1 - rest / c.splits;    // later rows see more: they start first
     const PagedSeq s = paged_seq(c.a, blockIdx.y);
-    const PagedTile t = paged_tile(c, s, tile, NB * 16);
+    if (s.n_rows * c.group > c.few_rows) return;                         // k_paged_chunk's
+    const PagedTile t = paged_tile<kKeyTile>(c, s, tile, NB * 16);
     if (t.rows == 0) return;
     const int per = max(c.split_tiles, (t.tiles + c.splits - 1) / c.splits), used = max(1, (t.tiles + per - 1) / per);
     if (split >= used) return;
@@ -606,12 +654,6 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedAttn c) {
     }
     __syncthreads();
     const size_t unit = ((size_t)blockIdx.y * c.a.n_kv + h) * c.row_tiles + tile;
-    auto finish = [&](int row, int d, float M, float L, float v) {
-        const int r = t.r0 + row, tok = r / c.group, qh = h * c.group + r % c.group;
-        const size_t at = (size_t)(s.row0 + tok) * c.out.row_stride + (size_t)qh * c.out.head_stride + d;
-        put_out<OT>(c, at, L == 0.f ? 0.f : v / L);
-        if (c.lse && d == 0) c.lse[(size_t)(s.row0 + tok) * c.n_heads + qh] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994531f;
-    };
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         float M = -INFINITY;
@@ -635,7 +677,7 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedAttn c) {
             for (int i = 0; i < HD / 16; ++i) {
                 const int d = i * 16 + ((int)threadIdx.x & 15);
                 const float v = ob[0][row][d] + ob[1][row][d] + ob[2][row][d] + ob[3][row][d];
-                if (used == 1) finish(b * 16 + row, d, R, L, v);
+                if (used == 1) paged_finish<OT>(c, s, t, h, b * 16 + row, d, R, L, v);
                 else st_coherent(c.part_o + ((unit * c.splits + split) * (NB * 16) + b * 16 + row) * HD + d, v);
             }
             if (used > 1 && ((int)threadIdx.x & 15) == 0) {
@@ -646,26 +688,8 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedAttn c) {
         }
     }
     if (used == 1) return;
-    wait_stores();
-    __syncthreads();
-    if (threadIdx.x == 0) last_one = __hip_atomic_fetch_add(c.tickets + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1;
-    __syncthreads();
-    if (!last_one) return;
-    if (threadIdx.x == 0) st_coherent(c.tickets + unit, 0);
-    for (int e = (int)threadIdx.x; e < t.rows * HD; e += 256) {
-        const int row = e / HD, d = e % HD;
-        const float *po = c.part_o + (unit * c.splits * (NB * 16) + row) * HD + d;
-        const float *pm = (const float *)(c.part_ml + unit * c.splits * (NB * 16) + row);
-        float M = -INFINITY, L = 0.f, v = 0.f;
-        for (int i = 0; i < used; ++i) M = fmaxf(M, ld_coherent(pm + (size_t)i * (NB * 16) * 2));
-        if (M != -INFINITY)
-            for (int i = 0; i < used; ++i) {
-                const float f = __builtin_amdgcn_exp2f(ld_coherent(pm + (size_t)i * (NB * 16) * 2) - M);
-                L += f * ld_coherent(pm + (size_t)i * (NB * 16) * 2 + 1);
-                v += f * ld_coherent(po + (size_t)i * (NB * 16) * HD);
-            }
-        finish(row, d, M, L, v);
-    }
+    if (!paged_last(c, unit, used, &last_one)) return;
+    paged_join<OT, HD>(c, s, t, h, unit, used, NB * 16);
 }
 
 }  // namespace ead

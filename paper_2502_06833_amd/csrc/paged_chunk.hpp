@@ -1,0 +1,335 @@
+// Attention of many rows per KV head over a paged cache: bf16 products on the matrix cores with K and V in LDS.
+#pragma once
+#include "paged.hpp"
+
+namespace ead {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kChunkKeys = 64;       // keys of a tile
+constexpr int kChunkRows = 128;      // rows of a workgroup, 32 to a wave
+
+// LDS holds a tile's rows of K (and of V) one after the other, their 16-byte pieces permuted by an exclusive or with a number of
+// the key's: the 16-byte reads of K (32 keys, one piece each) and the transposing 8-byte reads of V (four keys, 64 neighbouring
+// bytes each) then both touch every bank once.
+template <int HD> __device__ __forceinline__ int chunk_swizzle(int key) {
+    if (HD == 128) return ((key & 3) << 2) | ((key >> 2) & 3);
+    if (HD == 64) return (((key >> 1) & 1) << 2) | ((key >> 2) & 3);
+    return (key >> 2) & 3;
+}
+
+using lds_char = __attribute__((address_space(3))) char;
+
+// Four waves take 32 rows each of a tile of 128, all of them every tile of 64 keys, which lands in LDS while the one before is
+// worked on (a bf16 cache: straight from memory, 1 KB a request; an 8-bit cache: through registers, where it becomes bf16).
+//   S^T = K Q^T with 32x32x16 products: lane (n, h) = (lane & 31, lane >> 5) gets row n's scores for keys 8 i + 4 h + 0..3, i = 0..3, of a block
+//   of 32: its statistics are its own up to one exchange of the wave's halves, and the scores of 16 keys, rounded to bf16, are the
+//   operand that O^T = V^T P^T wants if V's keys are taken in the same order.  V^T's operand comes from LDS by transposing reads.
+//
+//  Probabilities enter the second product as bf16.  One term of each is off by up to 2^-8 of it, which beside the rounding of the output
+//  makes the result's error against 64 bits 0.0023 of its norm instead of 0.0017; a second term (what the first leaves, rounded) takes that away for
+//  half as many products again.  Rows at a mask's edge, among them all that see few keys, always have both; the other tiles have both where no row of
+//  the launch sees more than kPagedTwoTerms keys (TWO): 4096 rows over 12289 .. 16384 keys of 32 heads take 1050 us with one term, 1400 with two.
+template <typename CT, int HD, bool TWO>
+__global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
+    constexpr bool F8 = sizeof(CT) == 1;
+    constexpr int kRowBytes = HD * 2, kHalf = kChunkKeys * kRowBytes, kBuf = 2 * kHalf;    // K, then V
+    constexpr int KS = HD / 16, CB = HD / 32;
+    constexpr int kReq = HD / 32;                                        // direct requests per wave, tile and operand
+    constexpr int EB = HD / 4 < 16 ? HD / 4 : 16, NL = HD / 4 / EB;      // 8-bit: bytes of a load, loads per lane, tile and operand
+    __shared__ __align__(1024) char lds[2 * kBuf];
+    __shared__ int last_one;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int n = lane & 31, hh = lane >> 5;
+    const int h = (int)blockIdx.x % c.a.n_kv, rest = (int)blockIdx.x / c.a.n_kv;
+    const int split = rest % c.splits, tile = c.row_tiles - 1 - rest / c.splits;
+    const PagedSeq s = paged_seq(c.a, blockIdx.y);
+    if (s.n_rows * c.group <= c.few_rows) return;                        // k_paged_attn's
+    const PagedTile t = paged_tile<kChunkKeys>(c, s, tile, kChunkRows);
+    if (t.rows == 0) return;
+    const int per = max(c.split_tiles, (t.tiles + c.splits - 1) / c.splits), used = max(1, (t.tiles + per - 1) / per);
+    if (split >= used) return;
+    const int begin = split * per, count = min(begin + per, t.tiles) - begin;
+
+    // this wave's rows, and this lane's
+    const int w0 = t.r0 + 32 * wave, w_rows = min(max(t.r0 + t.rows - w0, 0), 32);
+    const int p_lo = s.first + w0 / c.group, p_hi = s.first + (w0 + max(w_rows, 1) - 1) / c.group;
+    const int my_tok = (w0 + n) / c.group, my_head = h * c.group + (w0 + n) % c.group, my_pos = s.first + my_tok;
+    bf16x8_t q[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+        u32x4_t x = {0u, 0u, 0u, 0u};
+        if (n < w_rows) {
+            const bf16_t *p = (const bf16_t *)c.q.p + (size_t)(s.row0 + my_tok) * c.q.row_stride + (size_t)my_head * c.q.head_stride + 16 * i + 8 * hh;
+            if (c.q.vec) x = *(gptr<u32x4_t>)p;
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = (uint32_t)p[2 * e].u | (uint32_t)p[2 * e + 1].u << 16;
+        }
+        q[i] = __builtin_bit_cast(bf16x8_t, x);
+    }
+    f32x16_t o[CB];
+#pragma unroll
+    for (int i = 0; i < CB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    // where this lane reads: K's piece 2 i + hh of key n; V's four elements of keys 4 hh + (lane & 15) / 4 (+ 8)
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_char *)lds;
+    uint32_t k_at[KS], v_at[CB][2];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) k_at[i] = base + n * kRowBytes + (((2 * i + hh) ^ chunk_swizzle<HD>(n)) << 4);
+#pragma unroll
+    for (int i = 0; i < CB; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int key = 8 * e + 4 * hh + ((lane & 15) >> 2), piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+            v_at[i][e] = base + kHalf + key * kRowBytes + ((piece ^ chunk_swizzle<HD>(key)) << 4) + (lane & 1) * 8;
+        }
+
+    // ---- staging.  Wave w brings keys 16 w .. 16 w + 15 of every tile.  The pages of 16 tiles are looked up at a time (lane 4 i + g: tile i, keys 16 g).
+    const int page_mask = (1 << c.a.page_shift) - 1;
+    auto key_base = [&](int i) { const int v = begin + i; return (v < t.n_sink ? v : v - t.n_sink + t.t_lo) * kChunkKeys; };
+    auto look_up = [&](int i0) {
+        const int i = i0 + (lane >> 2);
+        if (i >= count) return -1;
+        const int pos = key_base(i) + 16 * (lane & 3);
+        return pos < s.kv ? paged_page(c.a, s, pos) : -1;
+    };
+    int pages = look_up(0), pages_next = count > 16 ? look_up(16) : -1;
+    uint64_t held = __ballot(pages >= 0);
+    int staged_valid = 0;                        // bit g: keys 16 g of the tile staged last have a page
+    Raw<EB> raw[2][F8 ? NL : 1];
+    uint32_t raw_scale[2][F8 ? NL : 1];
+    uint32_t from[kReq];
+    if constexpr (!F8) {
+#pragma unroll
+        for (int i = 0; i < kReq; ++i) {
+            const int at = i * 1024 + lane * 16, r = at / kRowBytes, piece = at % kRowBytes >> 4;
+            from[i] = r * kRowBytes + ((piece ^ chunk_swizzle<HD>(r)) << 4);
+        }
+    }
+    auto request = [&](int i) {
+        if ((i & 15) == 0 && i) {
+            pages = pages_next;
+            held = __ballot(pages >= 0);
+            pages_next = i + 16 < count ? look_up(i + 16) : -1;
+        }
+        staged_valid = (int)(held >> (4 * (i & 15))) & 15;
+        const int page = max(__builtin_amdgcn_readlane(pages, 4 * (i & 15) + wave), 0), pos = key_base(i) + 16 * wave;
+        const size_t vec = paged_vec(c.a, page, h, pos & page_mask);
+        if constexpr (F8) {
+            const uint8_t *src[2] = {(const uint8_t *)c.a.k + vec * HD, (const uint8_t *)c.a.v + vec * HD};
+            const uint8_t *scale[2] = {c.a.ks + vec, c.a.vs + vec};
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+                for (int e = 0; e < NL; ++e) {
+                    const int at = (e * 64 + lane) * EB;
+                    raw[kv][e].load(src[kv] + at);
+                    raw_scale[kv][e] = *(gptr<uint8_t>)(scale[kv] + at / HD);
+                }
+        } else {
+            const uint32_t to = base + (i & 1) * kBuf + wave * 16 * kRowBytes;
+#pragma unroll
+            for (int e = 0; e < kReq; ++e) request_tile((const bf16_t *)c.a.k + vec * HD, from[e], to + e * 1024);
+#pragma unroll
+            for (int e = 0; e < kReq; ++e) request_tile((const bf16_t *)c.a.v + vec * HD, from[e], to + kHalf + e * 1024);
+        }
+    };
+    auto place = [&](int i) {                    // 8-bit: the requested tile to LDS, as bf16
+        if constexpr (F8) {
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+                for (int e = 0; e < NL; ++e) {
+                    const int at = (e * 64 + lane) * EB, r = at / HD, piece = at % HD >> 3;
+                    const float f = exp2_of((int)raw_scale[kv][e]);
+                    const uint32_t row = base + (i & 1) * kBuf + kv * kHalf + (wave * 16 + r) * kRowBytes;
+#pragma unroll
+                    for (int x = 0; x < EB / 8; ++x) {
+                        const uint32_t a = raw[kv][e].w[2 * x], b = raw[kv][e].w[2 * x + 1];
+                        *(__attribute__((address_space(3))) u32x4_t *)(uintptr_t)(row + (((piece + x) ^ chunk_swizzle<HD>(r)) << 4)) =
+                            u32x4_t{fp8_bf16x2<false>(a, f), fp8_bf16x2<true>(a, f), fp8_bf16x2<false>(b, f), fp8_bf16x2<true>(b, f)};
+                    }
+                }
+        }
+    };
+
+    auto work = [&](int i, int valid, auto edge_c) {
+        constexpr bool EDGE = decltype(edge_c)::value;
+        const uint32_t buf = (i & 1) * kBuf;
+        const int key0 = key_base(i);
+        f32x16_t sc[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
+#pragma unroll
+            for (int e = 0; e < KS; ++e) {
+                const bf16x8_t k = *(__attribute__((address_space(3))) bf16x8_t *)(uintptr_t)(k_at[e] + buf + b * 32 * kRowBytes);
+                sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[e], sc[b], 0, 0, 0);
+            }
+        }
+        if constexpr (EDGE) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int key = key0 + 32 * b + 8 * (e >> 2) + 4 * hh + (e & 3);
+                    sc[b][e] = (valid >> (2 * b + (e >> 3)) & 1) && paged_sees(c, my_pos, key) ? sc[b][e] : -INFINITY;
+                }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[b][e]);
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c.c2;
+        if (__any(top > m + 8.f)) {
+            const float to = top > m + 8.f ? top : m, f = top > m + 8.f ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int x = 0; x < CB; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[x][e] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        constexpr bool kLow = TWO || EDGE;
+        uint32_t p[2][8], p_lo[2][8];            // the probabilities' bf16 terms
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e], c.c2, -ref)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e + 1], c.c2, -ref));
+                l += x + y;
+                p[b][e] = pack_bf16(x, y);
+                if constexpr (kLow) p_lo[b][e] = pack_bf16(x - __uint_as_float(p[b][e] << 16), y - __uint_as_float(p[b][e] & 0xFFFF0000u));
+            }
+        bool odd = false;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const u32x4_t pw = {p[b][4 * k], p[b][4 * k + 1], p[b][4 * k + 2], p[b][4 * k + 3]};
+                u32x4_t pl;
+                if constexpr (kLow) pl = u32x4_t{p_lo[b][4 * k], p_lo[b][4 * k + 1], p_lo[b][4 * k + 2], p_lo[b][4 * k + 3]};
+#pragma unroll
+                for (int x = 0; x < CB; ++x) {
+                    const uint32_t at = buf + (2 * b + k) * 16 * kRowBytes;
+                    using tr_t = __attribute__((address_space(3))) bf16x4_t;
+                    union { bf16x4_t v[2]; u32x4_t w; } a;
+                    a.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(v_at[x][0] + at));
+                    a.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(v_at[x][1] + at));
+                    if constexpr (EDGE) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool b0 = (a.w[e] & 0x7F80u) == 0x7F80u, b1 = (a.w[e] & 0x7F800000u) == 0x7F800000u;
+                            odd |= b0 || b1;
+                            a.w[e] &= (b0 ? 0xFFFF0000u : 0xFFFFFFFFu) & (b1 ? 0xFFFFu : 0xFFFFFFFFu);
+                        }
+                    }
+                    o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.w), __builtin_bit_cast(bf16x8_t, pw), o[x], 0, 0, 0);
+                    if constexpr (kLow) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.w), __builtin_bit_cast(bf16x8_t, pl), o[x], 0, 0, 0);
+                }
+            }
+        if constexpr (EDGE) {
+            if (__any(odd)) {
+                // infinities and NaN, left out of the product, go to the rows that see them (PagedWave::add_odd)
+                for (int k = 0; k < kChunkKeys; ++k) {
+                    const int key = key0 + k;
+                    if (!(valid >> (k >> 4) & 1) || key > p_hi) continue;
+                    const size_t vec = paged_vec(c.a, paged_page(c.a, s, key), h, key & page_mask);
+                    const bool sees = n < w_rows && paged_sees(c, my_pos, key);
+#pragma unroll
+                    for (int x = 0; x < CB; ++x)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const size_t at = vec * HD + 32 * x + 8 * (e >> 2) + 4 * hh + (e & 3);
+                            float v;
+                            if constexpr (F8) v = (((const uint8_t *)c.a.v)[at] & 0x7F) == 0x7F ? __builtin_nanf("") : 0.f;
+                            else v = to_f32(((const CT *)c.a.v)[at]);
+                            o[x][e] += sees && !(__builtin_fabsf(v) <= 3.402823466e38f) ? v : 0.f;
+                        }
+                }
+            }
+        }
+    };
+
+    if (count > 0) request(0);
+    if constexpr (F8) {
+        place(0);
+        if (count > 1) { /* the next tile's words wait in registers */ }
+    }
+    int valid = staged_valid;
+    if constexpr (F8) { if (count > 1) request(1); }
+    for (int i = 0; i < count; ++i) {
+        // tile i has landed for every wave, and every wave is done with the buffer of tile i - 1
+        if constexpr (F8) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        int valid_next = staged_valid;
+        if constexpr (!F8) {
+            if (i + 1 < count) request(i + 1);
+            valid_next = staged_valid;
+        }
+        const int key0 = key_base(i), last = key0 + kChunkKeys - 1;
+        const bool skip = w_rows == 0 || key0 > p_hi || (c.window && key0 >= c.sinks && p_lo - last >= c.window);
+        if (!skip) {
+            const bool whole = valid == 15 && last <= p_lo && (!c.window || p_hi - key0 < c.window || last < c.sinks);
+            if (whole) work(i, valid, std::false_type{});
+            else work(i, valid, std::true_type{});
+        }
+        if constexpr (F8) {
+            if (i + 1 < count) place(i + 1);
+            valid_next = staged_valid;
+            if (i + 2 < count) request(i + 2);
+        }
+        valid = valid_next;
+    }
+
+    // ---- the row's sum, and what goes out
+    const auto sums = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(sums[0]) + __uint_as_float(sums[1]);
+    if (l != l && m == -INFINITY) m = 0.f;
+    const size_t unit = ((size_t)blockIdx.y * c.a.n_kv + h) * c.row_tiles + tile;
+    if (used == 1) {
+        if (n >= w_rows) return;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bf16_t *p = (bf16_t *)c.out.p + (size_t)(s.row0 + my_tok) * c.out.row_stride + (size_t)my_head * c.out.head_stride;
+#pragma unroll
+        for (int x = 0; x < CB; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int d = 32 * x + 8 * e + 4 * hh;
+                const uint2 w = make_uint2(l == 0.f ? 0u : pack_bf16(o[x][4 * e] * inv, o[x][4 * e + 1] * inv), l == 0.f ? 0u : pack_bf16(o[x][4 * e + 2] * inv, o[x][4 * e + 3] * inv));
+                if (c.out.vec) *(uint2 *)(p + d) = w;
+                else {
+                    p[d].u = (uint16_t)w.x; p[d + 1].u = (uint16_t)(w.x >> 16);
+                    p[d + 2].u = (uint16_t)w.y; p[d + 3].u = (uint16_t)(w.y >> 16);
+                }
+            }
+        if (c.lse && hh == 0) c.lse[(size_t)(s.row0 + my_tok) * c.n_heads + my_head] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+        return;
+    }
+    const size_t slot = (unit * c.splits + split) * kChunkRows;
+    if (n < w_rows) {
+        float *p = c.part_o + (slot + 32 * wave + n) * HD;
+#pragma unroll
+        for (int x = 0; x < CB; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) st_coherent(p + 32 * x + 8 * (e >> 2) + 4 * hh + (e & 3), o[x][e]);
+        if (hh == 0) {
+            float *pm = (float *)(c.part_ml + slot + 32 * wave + n);
+            st_coherent(pm, m);
+            st_coherent(pm + 1, l);
+        }
+    }
+    if (!paged_last(c, unit, used, &last_one)) return;
+    paged_join<bf16_t, HD>(c, s, t, h, unit, used, kChunkRows);
+}
+
+}  // namespace ead
