@@ -151,7 +151,7 @@ PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_
     p.few = f32 || (long)b->min_q * group <= kPagedFewRows;
     p.many = !f32 && rows > kPagedFewRows;
     if (p.few) p.f = paged_few(b->batch, c->n_kv_heads, group, f32 ? rows : std::min(rows, (long)kPagedFewRows), held, at->window, at->sinks, cus, paged_max_blocks(f32, c->head_dim));
-    if (p.many) p.m = paged_many(b->batch, c->n_kv_heads, group, rows, held, at->window, at->sinks, cus);
+    if (p.many) p.m = paged_many(b->batch, c->n_kv_heads, group, rows, held, at->window, at->sinks, cus, c->head_dim);
     p.two = paged_keys(128, 64, group, held, at->window, at->sinks) <= kPagedTwoTerms;
     p.f_bytes = p.few ? paged_bytes(p.f, c->head_dim) : 0;
     p.m_bytes = p.many ? paged_bytes(p.m, c->head_dim) : 0;
@@ -213,6 +213,7 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     const hipStream_t st = (hipStream_t)hip_stream;
     if (p.few) {
         const dim3 grid = set_plan(c, p.f, (char *)workspace, batch->batch);
+        c.once = p.f.row_tiles == 1;
         with_cache(cache, [&](auto ct, auto hd) {
             using CT = decltype(ct);
             constexpr int HD = decltype(hd)::value;

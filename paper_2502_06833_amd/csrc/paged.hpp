@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "paged_rules.hpp"
 
 namespace ead {
 
@@ -214,6 +215,7 @@ struct PagedAttn {
     int n_heads, group;             // group: query heads per KV head
     float c2;                       // scale * log2(e): scores are kept in units of one bit
     int window, sinks;
+    int once;                       // every key is read by one workgroup: requests are non-temporal (request_tile)
     int few_rows;                   // sequences with at most this many rows per KV head are k_paged_attn's, the others k_paged_chunk's
     int row_tiles, splits, split_tiles;   // grid.x = row_tiles * splits * n_kv; at least split_tiles key tiles to a split
     float *part_o;                  // [unit][split][tile row][head_dim], relative to the split's maximum
@@ -267,40 +269,60 @@ template <int N> struct Raw {
     }
 };
 
-// One wave's piece of attention: a tile of 32 keys against NB blocks of 16 rows, everything in registers.
+// ---- LDS by its address ----------------------------------------------------------------------------
+using lds_byte = __attribute__((address_space(3))) char;
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(lds_byte *)p; }
+template <typename T> __device__ __forceinline__ T lds_read(uint32_t at) { return *(__attribute__((address_space(3))) T *)(uintptr_t)at; }
+// 4 bytes per lane, each from its own address, to LDS at lds + 4 lane (M0 as in request_tile)
+__device__ __forceinline__ void request_words(const void *p, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+// 16 bytes per lane likewise, to lds + 16 lane
+__device__ __forceinline__ void request_pieces(const void *p, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+template <int N> __device__ __forceinline__ void wait_requests() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Rows of K and V (one key each, ROW bytes) lie one after the other in LDS, their 16-byte pieces permuted by an exclusive or with this
+// number of the key: the 16-byte reads of K (one piece of 16 or 32 keys) and the transposing reads of V (4 or 8 keys, a few neighbouring
+// pieces each) then touch every bank as often as any other.
+template <int ROW> __device__ __forceinline__ int lds_swizzle(int key) {
+    if (ROW >= 256) return ((key & 3) << 2) | ((key >> 2) & 3);
+    if (ROW == 128) return (((key >> 1) & 1) << 2) | ((key >> 2) & 3);
+    if (ROW == 64) return (key >> 2) & 3;
+    return (key >> 3) & 1;
+}
+
+// One wave's piece of attention: tiles of 32 keys against NB blocks of 16 rows.
 //
+//  Tiles come to a ring in LDS that is the wave's own, in requests of 1 KB of neighbouring bytes: no barrier, no registers, and whole
+//  cache lines (loads in the products' operand layout, 64 bytes of a key at a time, ran at 4.9 TB/s where these reach 6.8).
 //  S^T = K Q^T: the keys are the M of the product, rows the N, so lane (n, g) = (lane & 15, lane >> 4) gets the scores of row n
-//  for keys 4g .. 4g+3 of each half of the tile: statistics are the lane's own up to two shuffles over g, and the lane
+//  for keys 4g .. 4g+3 of each half of the tile: statistics are the lane's own up to two exchanges over g, and the lane
 //  already holds what the second product, O^T = V^T P^T, wants of P: its contraction runs over the keys in the order
-//  (j < 4 ? 4g + j : 16 + 4g + j - 4), in which V's rows are loaded.  V's M order is free too: lane n loads VW = HD/16
-//  neighbouring elements of each of its eight keys, the products c = 0 .. VW-1 take element c of every lane, and a
-//  lane ends up with the HD/4 neighbouring output elements VW (4g + r) + c of row n.  Turning eight
-//  keys x VW elements into VW operands is one byte permute per word; nothing goes through LDS.
+//  (j < 4 ? 4g + j : 16 + 4g + j - 4), in which V's transposing reads from LDS take them.  Float V needs no transposing: there a lane
+//  reads VW neighbouring elements of each of its keys, and product c takes element c of every lane.
 template <typename CT, int HD, int NB>
 struct PagedWave {
     static constexpr bool F32 = sizeof(CT) == 4, F8 = sizeof(CT) == 1;
-    static constexpr int VW = F32 ? (HD / 16 < 4 ? HD / 16 : 4) : HD / 16;   // neighbouring elements of V in one load
-    static constexpr int VC = HD / 16 / VW;                                  // loads per key (2 for float, HD 128)
-    // K's contraction order is free as long as Q's is the same: a lane takes KE neighbouring elements at a time
-    static constexpr int KE = F32 ? 4 : F8 ? (HD >= 64 ? 16 : 8) : 8;
-    static constexpr int KL = HD / 4 / KE;                                   // loads per key
+    static constexpr int kRow = HD * (int)sizeof(CT);                        // bytes of a key
+    static constexpr int kPart = kKeyTile * kRow, kTile = 2 * kPart + (F8 ? 256 : 0);   // K, V, exponents
+    static constexpr int kReq = 16 * kRow / 1024 > 0 ? 16 * kRow / 1024 : 1;  // requests for 16 keys of K or V (8-bit HD 32: for 32 keys)
+    static constexpr bool kShort = 16 * kRow < 1024;
+    static constexpr int kRequests = (kShort ? 2 : 4 * kReq) + (F8 ? 1 : 0);  // for a tile
+    static constexpr int kRing = kTile > 16384 + 256 ? 1 : kTile * 2 > 8192 ? 2 : 8192 / kTile;   // tiles
+    static constexpr int VW = HD / 16 < 4 ? HD / 16 : 4;                     // float: neighbouring elements of V in one read
+    static constexpr int KE = F32 ? 4 : F8 ? (HD >= 64 ? 16 : 8) : 8;        // neighbouring elements of K in one read
+    static constexpr int KL = HD / 4 / KE;                                   // reads per key
     static constexpr int QW = F32 ? HD / 4 : HD / 8;                         // words of Q per lane
-
-    // a second tile's words fit beside the queries, the outputs and the scores
-    static constexpr bool kAhead = 2 * (HD / 2) * (int)sizeof(CT) / 2 + NB * (QW + HD / 4 + 16) <= 264;
 
     uint32_t q[NB][QW];
     f32x4_t o[NB][HD / 16];
     float m[NB], l[NB];             // in bits; l: this lane's keys only
+    uint32_t from[kReq], k_at[KL], v_at[F32 ? 1 : HD / 16];
 
-    struct Keys {                   // what a wave has requested of a tile
-        Raw<KE * (int)sizeof(CT)> k[2][KL];
-        Raw<VW * (int)sizeof(CT)> v[8][VC];
-        uint32_t ks[2], vs[2];      // exponents: K of key n of each half; V of keys 4g..4g+3 of each half
-        int base;                   // first position
-        int page[2];                // of each half; -1: a hole or past the end
-    };
-
+    // element KE (4 i + g) + .. of the row's queries belongs to K's read i: the contraction's order is free as long as both have the same
     __device__ __forceinline__ void init(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int lane) {
         const int n = lane & 15, g = lane >> 4;
 #pragma unroll
@@ -317,7 +339,7 @@ struct PagedWave {
                 const size_t at = (size_t)(s.row0 + tok) * c.q.row_stride + (size_t)qh * c.q.head_stride;
 #pragma unroll
                 for (int i = 0; i < KL; ++i) {
-                    const int d = i * 4 * KE + g * KE;
+                    const int d = (4 * i + g) * KE;
                     if constexpr (F32) {
                         const float *p = (const float *)c.q.p + at + d;
                         if (c.q.vec) { Raw<16> x; x.load(p); for (int e = 0; e < 4; ++e) q[b][i * 4 + e] = x.w[e]; }
@@ -330,35 +352,58 @@ struct PagedWave {
                 }
             }
         }
-    }
-
-    // Every address is inside the pool: halves without a page (holes, positions past the end) read page 0 and are masked
-    __device__ __forceinline__ void load(const PagedAttn &c, const PagedSeq &s, int tile, int h, int lane, Keys &x) const {
-        const int n = lane & 15, g = lane >> 4;
-        x.base = tile * kKeyTile;
-        const int mask = (1 << c.a.page_shift) - 1;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int pos = x.base + 16 * half;
-            x.page[half] = pos < s.kv ? paged_page(c.a, s, pos) : -1;
-            const size_t vec = paged_vec(c.a, max(x.page[half], 0), h, pos & mask);
-            const CT *k = (const CT *)c.a.k + vec * HD, *v = (const CT *)c.a.v + vec * HD;
+        for (int e = 0; e < kReq; ++e) {                     // where this lane's piece of a request lies among 16 keys
+            const int at = e * 1024 + lane * 16, key = at / kRow, piece = at % kRow >> 4;
+            from[e] = (kShort ? key & 15 : key) * kRow + ((piece ^ lds_swizzle<kRow>(key)) << 4);
+        }
 #pragma unroll
-            for (int i = 0; i < KL; ++i) x.k[half][i].load(k + n * HD + i * 4 * KE + g * KE);
+        for (int i = 0; i < KL; ++i) {
+            const int byte = (4 * i + g) * KE * (int)sizeof(CT);
+            k_at[i] = n * kRow + (((byte >> 4) ^ lds_swizzle<kRow>(n)) << 4) + (byte & 15);
+        }
+        if constexpr (!F32) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < VC; ++i) x.v[half * 4 + j][i].load(v + (4 * g + j) * HD + i * 16 * VW + n * VW);
-            if constexpr (F8) {
-                x.ks[half] = *(gptr<uint8_t>)(c.a.ks + vec + n);
-                x.vs[half] = *(gptr<uint32_t>)(c.a.vs + vec + 4 * g);
+            for (int i = 0; i < HD / 16; ++i) {
+                const int key = F8 ? key_of(0, n >> 1, g) : 4 * g + (n >> 2), byte = F8 ? 16 * i + 8 * (n & 1) : 32 * i + 8 * (n & 3);
+                v_at[i] = kPart + key * kRow + (((byte >> 4) ^ lds_swizzle<kRow>(key)) << 4) + (byte & 15);
             }
         }
     }
 
+    // Requests a tile.  Every address is inside the pool: halves without a page (-1: holes, positions past the end) read page 0 and are masked
+    template <bool ONCE>
+    __device__ __forceinline__ void request(const PagedAttn &c, int base, int page0, int page1, int h, int lane, uint32_t to) const {
+        const int mask = (1 << c.a.page_shift) - 1;
+        const size_t vec0 = paged_vec(c.a, max(page0, 0), h, base & mask), vec1 = paged_vec(c.a, max(page1, 0), h, (base + 16) & mask);
+        if constexpr (kShort) {
+            const size_t at = (lane < 32 ? vec0 : vec1) * kRow + from[0];
+            request_pieces((const char *)c.a.k + at, to);
+            request_pieces((const char *)c.a.v + at, to + kPart);
+        } else {
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const char *p = (const char *)(part ? c.a.v : c.a.k);
+#pragma unroll
+                for (int e = 0; e < kReq; ++e) request_tile<ONCE>((const bf16_t *)(p + vec0 * kRow), from[e], to + part * kPart + e * 1024);
+#pragma unroll
+                for (int e = 0; e < kReq; ++e) request_tile<ONCE>((const bf16_t *)(p + vec1 * kRow), from[e], to + part * kPart + (kReq + e) * 1024);
+            }
+        }
+        // words 0..7: exponents of K, 8..15: of V (the other lanes repeat them)
+        if constexpr (F8) request_words((lane & 8 ? c.a.vs : c.a.ks) + (lane & 4 ? vec1 : vec0) + 4 * (lane & 3), to + 2 * kPart);
+    }
+
     __device__ __forceinline__ static int key_of(int base, int j, int g) { return base + (j < 4 ? 4 * g + j : 12 + 4 * g + j); }
 
-    __device__ __forceinline__ void take(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int lane, Keys &x) {
+    // Whether every row of the tile sees all of these keys
+    __device__ __forceinline__ static bool whole(const PagedAttn &c, const PagedTile &t, int base, int page0, int page1) {
+        const int last = base + kKeyTile - 1;
+        return page0 >= 0 && page1 >= 0 && last <= t.p_lo && (!c.window || t.p_hi - base < c.window || last < c.sinks);
+    }
+
+    template <bool EDGE>
+    __device__ __forceinline__ void take(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int lane, int base, int page0, int page1, uint32_t at) {
         const int n = lane & 15, g = lane >> 4;
         // ---- scores
         f32x4_t sc[NB][2];
@@ -366,25 +411,27 @@ struct PagedWave {
         for (int half = 0; half < 2; ++half) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) sc[b][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            float ks = 1.f;
+            if constexpr (F8) ks = exp2_of((int)lds_read<uint8_t>(at + 2 * kPart + 16 * half + n));
 #pragma unroll
             for (int i = 0; i < KL; ++i) {
+                const uint32_t k_from = at + k_at[i] + half * 16 * kRow;
                 if constexpr (F32) {
+                    const f32x4_t k = lds_read<f32x4_t>(k_from);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
-                            sc[b][half] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.k[half][i].w[e]), __uint_as_float(q[b][i * 4 + e]), sc[b][half], 0, 0, 0);
+                            sc[b][half] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], __uint_as_float(q[b][i * 4 + e]), sc[b][half], 0, 0, 0);
                 } else {
+                    uint32_t k[4];
+                    if constexpr (KE * sizeof(CT) == 8) { const u32x2_t x = lds_read<u32x2_t>(k_from); k[0] = x.x; k[1] = x.y; }
+                    else { const u32x4_t x = lds_read<u32x4_t>(k_from); k[0] = x.x; k[1] = x.y; k[2] = x.z; k[3] = x.w; }
 #pragma unroll
                     for (int e = 0; e < KE / 8; ++e) {
                         u32x4_t kw;
-                        if constexpr (F8) {
-                            const float ks = exp2_of((int)x.ks[half]);
-                            kw = u32x4_t{fp8_bf16x2<false>(x.k[half][i].w[2 * e], ks), fp8_bf16x2<true>(x.k[half][i].w[2 * e], ks),
-                                         fp8_bf16x2<false>(x.k[half][i].w[2 * e + 1], ks), fp8_bf16x2<true>(x.k[half][i].w[2 * e + 1], ks)};
-                        } else {
-                            kw = u32x4_t{x.k[half][i].w[0], x.k[half][i].w[1], x.k[half][i].w[2], x.k[half][i].w[3]};
-                        }
+                        if constexpr (F8) kw = u32x4_t{fp8_bf16x2<false>(k[2 * e], ks), fp8_bf16x2<true>(k[2 * e], ks), fp8_bf16x2<false>(k[2 * e + 1], ks), fp8_bf16x2<true>(k[2 * e + 1], ks)};
+                        else kw = u32x4_t{k[0], k[1], k[2], k[3]};
 #pragma unroll
                         for (int b = 0; b < NB; ++b) {
                             const int w = i * (KE / 2) + e * 4;
@@ -395,27 +442,14 @@ struct PagedWave {
                 }
             }
         }
-        // ---- masks: a tile that every row sees whole has none
-        const int last = x.base + kKeyTile - 1;
-        const bool whole = x.page[0] >= 0 && x.page[1] >= 0 && last <= t.p_lo && (!c.window || t.p_hi - x.base < c.window || last < c.sinks);
-        if (!whole) {
+        if constexpr (EDGE) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const int pos = s.first + (t.r0 + b * 16 + n) / c.group;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const bool sees = x.page[j >> 2] >= 0 && paged_sees(c, pos, key_of(x.base, j, g));
+                    const bool sees = (j < 4 ? page0 : page1) >= 0 && paged_sees(c, pos, key_of(base, j, g));
                     sc[b][j >> 2][j & 3] = sees ? sc[b][j >> 2][j & 3] : -INFINITY;
-                }
-            }
-            // V of keys that hold nothing any row sees: whatever lies there, 0 times it has to be 0
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int key = key_of(x.base, j, g);
-                const bool any = x.page[j >> 2] >= 0 && key <= t.p_hi && (!c.window || t.p_lo - key < c.window || key < c.sinks);
-                if (!any) {
-#pragma unroll
-                    for (int i = 0; i < VC; ++i) x.v[j][i].zero();
                 }
             }
         }
@@ -424,11 +458,11 @@ struct PagedWave {
         float p[NB][8];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, sc[b][j >> 2][j & 3]);
-            top = fmaxf(top, __shfl_xor(top, 16, kWave));
-            top = fmaxf(top, __shfl_xor(top, 32, kWave)) * c.c2;
+            float top = fmaxf(fmaxf(fmaxf(sc[b][0][0], sc[b][0][1]), fmaxf(sc[b][0][2], sc[b][0][3])), fmaxf(fmaxf(sc[b][1][0], sc[b][1][1]), fmaxf(sc[b][1][2], sc[b][1][3])));
+            const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
+            const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1])) * c.c2;
             if (__any(top > m[b] + 8.f)) {           // rows that need none keep theirs: what a row gets is its own affair
                 const float to = top > m[b] + 8.f ? top : m[b], f = top > m[b] + 8.f ? __builtin_amdgcn_exp2f(m[b] - to) : 1.f;
                 m[b] = to;
@@ -440,37 +474,44 @@ struct PagedWave {
             }
             const float ref = m[b] == -INFINITY ? 0.f : m[b];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                p[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][j >> 2][j & 3], c.c2, -ref));
-                l[b] += p[b][j];
-            }
+            for (int j = 0; j < 8; ++j) p[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][j >> 2][j & 3], c.c2, -ref));
+            l[b] += ((p[b][0] + p[b][1]) + (p[b][2] + p[b][3])) + ((p[b][4] + p[b][5]) + (p[b][6] + p[b][7]));
         }
-        // ---- output
+        // ---- output.  At an edge, infinities and NaN among the values are left out of the product (0 times what a row does not see
+        // has to be 0, whatever lies there) and added to the rows that see them.
+        bool odd = false;
         if constexpr (F32) {
-            bool odd = false;
-            if (!whole) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int i = 0; i < VC; ++i)
-#pragma unroll
-                        for (int e = 0; e < VW; ++e) {
-                            const bool bad = (x.v[j][i].w[e] & 0x7F800000u) == 0x7F800000u;
-                            odd |= bad;
-                            x.v[j][i].w[e] = bad ? 0u : x.v[j][i].w[e];
-                        }
-            }
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int i = 0; i < VC; ++i)
+                for (int i = 0; i < HD / 16 / VW; ++i) {
+                    const int key = key_of(0, j, g), byte = 4 * VW * (16 * i + n);
+                    const uint32_t v_from = at + kPart + key * kRow + (((byte >> 4) ^ lds_swizzle<kRow>(key)) << 4) + (byte & 15);
+                    uint32_t w[4];
+                    if constexpr (VW == 2) { const u32x2_t x = lds_read<u32x2_t>(v_from); w[0] = x.x; w[1] = x.y; }
+                    else { const u32x4_t x = lds_read<u32x4_t>(v_from); w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; }
 #pragma unroll
-                    for (int e = 0; e < VW; ++e)
+                    for (int e = 0; e < VW; ++e) {
+                        if constexpr (EDGE) {
+                            const bool bad = (w[e] & 0x7F800000u) == 0x7F800000u;
+                            odd |= bad;
+                            w[e] = bad ? 0u : w[e];
+                        }
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
-                            o[b][i * VW + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[j][i].w[e]), p[b][j], o[b][i * VW + e], 0, 0, 0);
-            if (__any(odd)) add_odd(c, s, t, h, lane, x);
+                            o[b][i * VW + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[e]), p[b][j], o[b][i * VW + e], 0, 0, 0);
+                    }
+                }
         } else {
+            if constexpr (F8) {                      // the values' powers of two go to the probabilities: exact
+                const uint32_t s0 = lds_read<uint32_t>(at + 2 * kPart + 32 + 4 * g), s1 = lds_read<uint32_t>(at + 2 * kPart + 48 + 4 * g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float vs = exp2_of((int)(((j < 4 ? s0 : s1) >> (8 * (j & 3))) & 0xFFu));
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) p[b][j] = EDGE && p[b][j] == 0.f ? 0.f : p[b][j] * vs;
+                }
+            }
             // two bf16 terms of every probability
             u32x4_t hi[NB], lo[NB];
 #pragma unroll
@@ -478,55 +519,50 @@ struct PagedWave {
                 hi[b] = __builtin_bit_cast(u32x4_t, take_bf16(p[b]));
                 lo[b] = u32x4_t{pack_bf16(p[b][0], p[b][1]), pack_bf16(p[b][2], p[b][3]), pack_bf16(p[b][4], p[b][5]), pack_bf16(p[b][6], p[b][7])};
             }
-            bool odd = false;
 #pragma unroll
-            for (int d = 0; d < VW / 2; ++d) {
-                uint32_t w[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if constexpr (F8) {
-                        const float vs = exp2_of((int)((x.vs[j >> 2] >> (8 * (j & 3))) & 0xFFu));
-                        const uint32_t word = x.v[j][0].w[d >> 1];
-                        w[j] = (d & 1) ? fp8_bf16x2<true>(word, vs) : fp8_bf16x2<false>(word, vs);
-                    } else {
-                        w[j] = x.v[j][0].w[d];
-                    }
+            for (int i = 0; i < HD / 16; ++i) {
+                u32x4_t v;
+                if constexpr (F8) {
+                    typedef int i32x2_t __attribute__((ext_vector_type(2)));
+                    const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t *)(uintptr_t)(at + v_at[i]));
+                    v = u32x4_t{fp8_bf16x2<false>((uint32_t)x.x, 1.f), fp8_bf16x2<true>((uint32_t)x.x, 1.f), fp8_bf16x2<false>((uint32_t)x.y, 1.f), fp8_bf16x2<true>((uint32_t)x.y, 1.f)};
+                } else {
+                    typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+                    using tr_t = __attribute__((address_space(3))) bf16x4_t;
+                    union { bf16x4_t x[2]; u32x4_t w; } a;
+                    a.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(at + v_at[i]));
+                    a.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(at + v_at[i] + 16 * kRow));
+                    v = a.w;
                 }
-                if (!whole) {
+                if constexpr (EDGE) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool b0 = (w[j] & 0x7F80u) == 0x7F80u, b1 = (w[j] & 0x7F800000u) == 0x7F800000u;
+                    for (int e = 0; e < 4; ++e) {
+                        const bool b0 = (v[e] & 0x7F80u) == 0x7F80u, b1 = (v[e] & 0x7F800000u) == 0x7F800000u;
                         odd |= b0 || b1;
-                        w[j] &= (b0 ? 0xFFFF0000u : 0xFFFFFFFFu) & (b1 ? 0xFFFFu : 0xFFFFFFFFu);
+                        v[e] &= (b0 ? 0xFFFF0000u : 0xFFFFFFFFu) & (b1 ? 0xFFFFu : 0xFFFFFFFFu);
                     }
-                }
-                u32x4_t va, vb;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    va[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
-                    vb[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
                 }
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    o[b][2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, hi[b]), o[b][2 * d], 0, 0, 0);
-                    o[b][2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vb), __builtin_bit_cast(bf16x8_t, hi[b]), o[b][2 * d + 1], 0, 0, 0);
-                    o[b][2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, lo[b]), o[b][2 * d], 0, 0, 0);
-                    o[b][2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vb), __builtin_bit_cast(bf16x8_t, lo[b]), o[b][2 * d + 1], 0, 0, 0);
+                    o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, hi[b]), o[b][i], 0, 0, 0);
+                    o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, lo[b]), o[b][i], 0, 0, 0);
                 }
             }
-            if (__any(odd)) add_odd(c, s, t, h, lane, x);
         }
+        if (EDGE && __any(odd)) add_odd(c, s, t, h, lane, base, page0, page1);
     }
 
     // Output element i (0 .. HD/16-1), r of this lane is dimension dim_of(i, r, g) of its row
-    __device__ __forceinline__ static int dim_of(int i, int r, int g) { return (i / VW) * 16 * VW + VW * (4 * g + r) + i % VW; }
+    __device__ __forceinline__ static int dim_of(int i, int r, int g) {
+        return F32 ? (i / VW) * 16 * VW + VW * (4 * g + r) + i % VW : 16 * i + 4 * g + r;
+    }
 
     // Infinities and NaN among the values of a tile that some rows see and others do not: they were left out of the
     // product, where a row that does not see them would have got 0 * NaN, and are added to the rows that do.
-    __device__ __forceinline__ void add_odd(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int lane, const Keys &x) {
+    __device__ __forceinline__ void add_odd(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int lane, int base, int page0, int page1) {
         const int n = lane & 15, g = lane >> 4;
         for (int k = 0; k < kKeyTile; ++k) {
-            const int key = x.base + k, page = k < 16 ? x.page[0] : x.page[1];
+            const int key = base + k, page = k < 16 ? page0 : page1;
             if (page < 0 || key > t.p_hi) continue;
             const size_t vec = paged_vec(c.a, page, h, key & ((1 << c.a.page_shift) - 1));
 #pragma unroll
@@ -572,21 +608,23 @@ __device__ __forceinline__ bool paged_last(const PagedAttn &c, size_t unit, int 
     return true;
 }
 
-// The parts of a unit joined: their order is that of the key ranges, whoever arrived last
+// The parts of a unit joined: their order is that of the key ranges, whoever arrived last.  `table`: LDS for used * t.rows maxima and sums.
 template <typename OT, int HD>
-__device__ __forceinline__ void paged_join(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, size_t unit, int used, int tile_rows) {
+__device__ __forceinline__ void paged_join(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, size_t unit, int used, int tile_rows, float2 *table) {
+    const float2 *pm = c.part_ml + unit * c.splits * tile_rows;
+    for (int e = (int)threadIdx.x; e < used * t.rows; e += 256) table[e] = pm[(size_t)(e / t.rows) * tile_rows + e % t.rows];
+    __syncthreads();
     for (int e = (int)threadIdx.x; e < t.rows * (HD / 4); e += 256) {
         const int row = e / (HD / 4), d = e % (HD / 4) * 4;
         const float *po = c.part_o + (unit * c.splits * tile_rows + row) * HD + d;
-        const float2 *pm = c.part_ml + unit * c.splits * tile_rows + row;
         float M = -INFINITY, L = 0.f;
         f32x4e_t v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 16
-        for (int i = 0; i < used; ++i) M = fmaxf(M, pm[(size_t)i * tile_rows].x);
+#pragma unroll 8
+        for (int i = 0; i < used; ++i) M = fmaxf(M, table[i * t.rows + row].x);
         const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll 16
         for (int i = 0; i < used; ++i) {
-            const float2 x = pm[(size_t)i * tile_rows];
+            const float2 x = table[i * t.rows + row];
             const float f = __builtin_amdgcn_exp2f(x.x - ref);
             L += f * x.y;
             v += f * *(const f32x4e_t *)(po + (size_t)i * tile_rows * HD);
@@ -597,16 +635,19 @@ __device__ __forceinline__ void paged_join(const PagedAttn &c, const PagedSeq &s
 }
 
 // Attention of few rows per KV head, and of float32 models' rows however many: a workgroup takes NB blocks of 16 rows of one
-// KV head and a range of keys, its four waves every fourth tile of the range.  K and V go from memory to
-// registers and into the matrix cores; a wave requests a tile while it works on the one before.  The waves' results
-// are joined through LDS, the ranges' by the workgroup that arrives last.
+// KV head and a range of keys, its four waves every fourth tile of the range.  The waves' results are joined through LDS, the ranges' by the
+// workgroup that arrives last.
 template <typename CT, int HD, int NB>
-__global__ __launch_bounds__(256) void k_paged_attn(PagedAttn c) {
+__global__ __launch_bounds__(256, (NB * HD < 256 && sizeof(CT) < 4) || HD == 32 ? 2 : 1) void k_paged_attn(PagedAttn c) {
     using W = PagedWave<CT, HD, NB>;
     using OT = typename std::conditional<sizeof(CT) == 4, float, bf16_t>::type;
-    __shared__ float ob[4][16][HD + 4];
+    constexpr int kWaveBytes = W::kRing * W::kTile, kJoin = 4 * 16 * (HD + 4) * 4;
+    constexpr int kTable = kPagedMaxSplits * NB * 16 * 8;
+    constexpr int kBytes = 4 * kWaveBytes > kJoin ? (4 * kWaveBytes > kTable ? 4 * kWaveBytes : kTable) : (kJoin > kTable ? kJoin : kTable);
+    __shared__ __align__(1024) char lds[kBytes];
     __shared__ float2 ml[4][NB * 16];
     __shared__ int last_one;
+    float (*ob)[16][HD + 4] = (float (*)[16][HD + 4])lds;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int h = (int)blockIdx.x % c.a.n_kv, rest = (int)blockIdx.x / c.a.n_kv;
     const int split = rest % c.splits, tile = c.row_tiles - 1 - rest / c.splits;    // later rows see more: they start first
@@ -620,26 +661,46 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedAttn c) {
 
     W w;
     w.init(c, s, t, h, lane);
-    auto key_tile = [&](int i) { return i < t.n_sink ? i : i - t.n_sink + t.t_lo; };
-    {
-        typename W::Keys x;
-        int i = begin + wave;
-        if constexpr (W::kAhead) {
-            typename W::Keys y;
-            if (i < end) w.load(c, s, key_tile(i), h, lane, x);
-            while (i < end) {
-                if (i + 4 < end) w.load(c, s, key_tile(i + 4), h, lane, y);
-                w.take(c, s, t, h, lane, x);
-                i += 4;
-                if (i >= end) break;
-                if (i + 4 < end) w.load(c, s, key_tile(i + 4), h, lane, x);
-                w.take(c, s, t, h, lane, y);
-                i += 4;
+    // This wave's tiles are begin + wave + 4 i, i < count.  Pages are looked up 32 tiles at a time: lane 2 i + half.
+    const int count = end - begin > wave ? (end - begin - wave + 3) / 4 : 0;
+    auto key_base = [&](int i) { const int v = begin + wave + 4 * i; return (v < t.n_sink ? v : v - t.n_sink + t.t_lo) * kKeyTile; };
+    auto look_up = [&](int i0) {
+        const int i = i0 + (lane >> 1);
+        if (i >= count) return -1;
+        const int pos = key_base(i) + 16 * (lane & 1);
+        return pos < s.kv ? paged_page(c.a, s, pos) : -1;
+    };
+    if (count > 0) {
+        // pages of the tiles being requested, of the next 32, and of the 32 that are worked on
+        int pages = look_up(0), pages_next = count > 32 ? look_up(32) : -1, pages_old = pages;
+        const uint32_t ring = lds_address(lds) + wave * kWaveBytes;
+        auto request = [&](int i) {
+            if ((i & 31) == 0 && i) {
+                pages_old = pages;
+                pages = pages_next;
+                pages_next = i + 32 < count ? look_up(i + 32) : -1;
             }
-        } else {
-            for (; i < end; i += 4) {
-                w.load(c, s, key_tile(i), h, lane, x);
-                w.take(c, s, t, h, lane, x);
+            const int p0 = __builtin_amdgcn_readlane(pages, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + 1);
+            const uint32_t to = ring + (i % W::kRing) * W::kTile;
+            if (c.once) w.template request<true>(c, key_base(i), p0, p1, h, lane, to);
+            else w.template request<false>(c, key_base(i), p0, p1, h, lane, to);
+        };
+#pragma unroll
+        for (int i = 0; i < W::kRing; ++i)
+            if (i < count) request(i);
+        int asked = min(count, W::kRing);
+        for (int i = 0; i < count; ++i) {
+            // of the tiles asked for, all but this one may still be on their way
+            if (asked - i >= W::kRing) wait_requests<(W::kRing - 1) * W::kRequests>();
+            else wait_requests<0>();
+            const int base = key_base(i), from = (asked - 1) >> 5 == i >> 5 ? pages : pages_old;
+            const int p0 = __builtin_amdgcn_readlane(from, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(from, 2 * (i & 31) + 1);
+            const uint32_t at = ring + (i % W::kRing) * W::kTile;
+            if (W::whole(c, t, base, p0, p1)) w.template take<false>(c, s, t, h, lane, base, p0, p1, at);
+            else w.template take<true>(c, s, t, h, lane, base, p0, p1, at);
+            if (asked < count) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // what was read of the tile is here: its place is free
+                request(asked++);
             }
         }
     }
@@ -689,7 +750,7 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedAttn c) {
     }
     if (used == 1) return;
     if (!paged_last(c, unit, used, &last_one)) return;
-    paged_join<OT, HD>(c, s, t, h, unit, used, NB * 16);
+    paged_join<OT, HD>(c, s, t, h, unit, used, NB * 16, (float2 *)lds);
 }
 
 }  // namespace ead

@@ -10,17 +10,6 @@ typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 constexpr int kChunkKeys = 64;       // keys of a tile
 constexpr int kChunkRows = 128;      // rows of a workgroup, 32 to a wave
 
-// LDS holds a tile's rows of K (and of V) one after the other, their 16-byte pieces permuted by an exclusive or with a number of
-// the key's: the 16-byte reads of K (32 keys, one piece each) and the transposing 8-byte reads of V (four keys, 64 neighbouring
-// bytes each) then both touch every bank once.
-template <int HD> __device__ __forceinline__ int chunk_swizzle(int key) {
-    if (HD == 128) return ((key & 3) << 2) | ((key >> 2) & 3);
-    if (HD == 64) return (((key >> 1) & 1) << 2) | ((key >> 2) & 3);
-    return (key >> 2) & 3;
-}
-
-using lds_char = __attribute__((address_space(3))) char;
-
 // Four waves take 32 rows each of a tile of 128, all of them every tile of 64 keys, which lands in LDS while the one before is
 // worked on (a bf16 cache: straight from memory, 1 KB a request; an 8-bit cache: through registers, where it becomes bf16).
 //   S^T = K Q^T with 32x32x16 products: lane (n, h) = (lane & 31, lane >> 5) gets row n's scores for keys 8 i + 4 h + 0..3, i = 0..3, of a block
@@ -38,6 +27,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
     constexpr int KS = HD / 16, CB = HD / 32;
     constexpr int kReq = HD / 32;                                        // direct requests per wave, tile and operand
     constexpr int EB = HD / 4 < 16 ? HD / 4 : 16, NL = HD / 4 / EB;      // 8-bit: bytes of a load, loads per lane, tile and operand
+    static_assert(paged_many_splits(HD) * kChunkRows * 8 <= 2 * kBuf, "the table of the join lies there too");
     __shared__ __align__(1024) char lds[2 * kBuf];
     __shared__ int last_one;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -77,16 +67,16 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
     float m = -INFINITY, l = 0.f;
 
     // where this lane reads: K's piece 2 i + hh of key n; V's four elements of keys 4 hh + (lane & 15) / 4 (+ 8)
-    const uint32_t base = (uint32_t)(uintptr_t)(lds_char *)lds;
+    const uint32_t base = lds_address(lds);
     uint32_t k_at[KS], v_at[CB][2];
 #pragma unroll
-    for (int i = 0; i < KS; ++i) k_at[i] = base + n * kRowBytes + (((2 * i + hh) ^ chunk_swizzle<HD>(n)) << 4);
+    for (int i = 0; i < KS; ++i) k_at[i] = base + n * kRowBytes + (((2 * i + hh) ^ lds_swizzle<kRowBytes>(n)) << 4);
 #pragma unroll
     for (int i = 0; i < CB; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int key = 8 * e + 4 * hh + ((lane & 15) >> 2), piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-            v_at[i][e] = base + kHalf + key * kRowBytes + ((piece ^ chunk_swizzle<HD>(key)) << 4) + (lane & 1) * 8;
+            v_at[i][e] = base + kHalf + key * kRowBytes + ((piece ^ lds_swizzle<kRowBytes>(key)) << 4) + (lane & 1) * 8;
         }
 
     // ---- staging.  Wave w brings keys 16 w .. 16 w + 15 of every tile.  The pages of 16 tiles are looked up at a time (lane 4 i + g: tile i, keys 16 g).
@@ -108,7 +98,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
 #pragma unroll
         for (int i = 0; i < kReq; ++i) {
             const int at = i * 1024 + lane * 16, r = at / kRowBytes, piece = at % kRowBytes >> 4;
-            from[i] = r * kRowBytes + ((piece ^ chunk_swizzle<HD>(r)) << 4);
+            from[i] = r * kRowBytes + ((piece ^ lds_swizzle<kRowBytes>(r)) << 4);
         }
     }
     auto request = [&](int i) {
@@ -151,7 +141,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
 #pragma unroll
                     for (int x = 0; x < EB / 8; ++x) {
                         const uint32_t a = raw[kv][e].w[2 * x], b = raw[kv][e].w[2 * x + 1];
-                        *(__attribute__((address_space(3))) u32x4_t *)(uintptr_t)(row + (((piece + x) ^ chunk_swizzle<HD>(r)) << 4)) =
+                        *(__attribute__((address_space(3))) u32x4_t *)(uintptr_t)(row + (((piece + x) ^ lds_swizzle<kRowBytes>(r)) << 4)) =
                             u32x4_t{fp8_bf16x2<false>(a, f), fp8_bf16x2<true>(a, f), fp8_bf16x2<false>(b, f), fp8_bf16x2<true>(b, f)};
                     }
                 }
@@ -329,7 +319,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
         }
     }
     if (!paged_last(c, unit, used, &last_one)) return;
-    paged_join<bf16_t, HD>(c, s, t, h, unit, used, kChunkRows);
+    paged_join<bf16_t, HD>(c, s, t, h, unit, used, kChunkRows, (float2 *)lds);
 }
 
 }  // namespace ead
