@@ -137,10 +137,37 @@ ead_status check_attention(const ead_paged_cache *cache, const ead_paged_batch *
     return EAD_OK;
 }
 
+// k_paged_attn for a cache and a number of blocks, and how many of its workgroups the device holds
+struct FewKernel {
+    void (*fn)(PagedAttn);
+    long resident;
+};
+template <typename CT, int HD, int NB> FewKernel few_kernel() {
+    static const int per_cu = [] {
+        int n = 0;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_paged_attn<CT, HD, NB>, 256, 0) != hipSuccess || n < 1) { (void)hipGetLastError(); n = 1; }
+        return n;
+    }();
+    return {k_paged_attn<CT, HD, NB>, (long)per_cu * compute_units()};
+}
+FewKernel few_kernel(const ead_paged_cache *c, int nb) {
+    FewKernel k{};
+    with_cache(c, [&](auto ct, auto hd) {
+        using CT = decltype(ct);
+        constexpr int HD = decltype(hd)::value;
+        if (nb == 1) k = few_kernel<CT, HD, 1>();
+        else if (nb == 2) k = few_kernel<CT, HD, 2>();
+        else if constexpr (paged_max_blocks(HD) == 4) k = few_kernel<CT, HD, 4>();
+    });
+    return k;
+}
+
 // The launches of a call: sequences with few rows (of a float32 cache: all), then those with many
 struct PagedCall {
     bool few, many, two;
-    PagedPlan f, m;
+    FewKernel kernel;
+    PagedShares f;
+    PagedPlan m;
     uint64_t f_bytes, m_bytes;
 };
 PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_paged_attn *at) {
@@ -148,23 +175,27 @@ PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_
     const bool f32 = c->dtype == EAD_F32;
     const long rows = (long)b->max_q * group;
     PagedCall p{};
-    p.few = f32 || (long)b->min_q * group <= kPagedFewRows;
-    p.many = !f32 && rows > kPagedFewRows;
-    if (p.few) p.f = paged_few(b->batch, c->n_kv_heads, group, f32 ? rows : std::min(rows, (long)kPagedFewRows), held, at->window, at->sinks, cus, paged_max_blocks(f32, c->head_dim));
-    if (p.many) p.m = paged_many(b->batch, c->n_kv_heads, group, rows, held, at->window, at->sinks, cus, c->head_dim);
-    p.two = paged_keys(128, 64, group, held, at->window, at->sinks) <= kPagedTwoTerms;
-    p.f_bytes = p.few ? paged_bytes(p.f, c->head_dim) : 0;
-    p.m_bytes = p.many ? paged_bytes(p.m, c->head_dim) : 0;
+    p.few = f32 || (long)b->min_q * group <= paged_few_rows(c->head_dim);
+    p.many = !f32 && rows > paged_few_rows(c->head_dim);
+    if (p.few) {
+        const long few = f32 ? rows : std::min(rows, (long)paged_few_rows(c->head_dim));
+        const int nb = paged_blocks(few, paged_max_blocks(c->head_dim));
+        p.kernel = few_kernel(c, nb);
+        p.f = paged_few(b->batch, c->n_kv_heads, few, nb, group, held, (long)b->table_width * c->page_size, at->window, at->sinks, p.kernel.resident);
+        p.f_bytes = paged_workspace(p.f.units, p.f.parts, 16 * nb, c->head_dim);
+    }
+    if (p.many) {
+        p.m = paged_many(b->batch, c->n_kv_heads, group, rows, held, at->window, at->sinks, cus, c->head_dim);
+        p.two = paged_keys(128, 64, group, held, at->window, at->sinks) <= kPagedTwoTerms;
+        p.m_bytes = paged_workspace(p.m.units, p.m.splits > 1 ? p.m.units * p.m.splits : 0, p.m.tile_rows, c->head_dim);
+    }
     return p;
 }
 
-// the plan and its part of the workspace
-dim3 set_plan(PagedAttn &c, const PagedPlan &p, char *ws, int batch) {
-    c.row_tiles = p.row_tiles; c.splits = p.splits; c.split_tiles = p.split_tiles;
+void set_workspace(PagedAttn &c, void *ws, long units, long parts, int tile_rows) {
     c.tickets = (int *)ws;
-    c.part_ml = (float2 *)(ws + (p.units + 63) / 64 * 256);
-    c.part_o = (float *)(c.part_ml + (size_t)p.units * p.splits * p.tile_rows);
-    return dim3((unsigned)((long)p.row_tiles * p.splits * c.a.n_kv), (unsigned)batch);
+    c.part_ml = (float2 *)((char *)ws + (units + 63) / 64 * 256);
+    c.part_o = (float *)(c.part_ml + (size_t)parts * tile_rows);
 }
 
 }  // namespace
@@ -209,21 +240,18 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     c.window = attn->window;
     c.sinks = attn->sinks;
     const bool f32 = cache->dtype == EAD_F32;
-    c.few_rows = f32 ? 0x7FFFFFFF : kPagedFewRows;
+    c.few_rows = f32 ? 0x7FFFFFFF : paged_few_rows(cache->head_dim);
     const hipStream_t st = (hipStream_t)hip_stream;
     if (p.few) {
-        const dim3 grid = set_plan(c, p.f, (char *)workspace, batch->batch);
+        set_workspace(c, workspace, p.f.units, p.f.parts, 16 * p.f.nb);
+        c.row_tiles = p.f.row_tiles; c.pairs = p.f.pairs; c.shares = (int)p.f.groups; c.min_share = p.f.min_share;
         c.once = p.f.row_tiles == 1;
-        with_cache(cache, [&](auto ct, auto hd) {
-            using CT = decltype(ct);
-            constexpr int HD = decltype(hd)::value;
-            if (p.f.tile_rows == 16) hipLaunchKernelGGL((k_paged_attn<CT, HD, 1>), grid, dim3(256), 0, st, c);
-            else if (p.f.tile_rows == 32) hipLaunchKernelGGL((k_paged_attn<CT, HD, 2>), grid, dim3(256), 0, st, c);
-            else if constexpr (paged_max_blocks(sizeof(CT) == 4, HD) == 4) hipLaunchKernelGGL((k_paged_attn<CT, HD, 4>), grid, dim3(256), 0, st, c);
-        });
+        hipLaunchKernelGGL(p.kernel.fn, dim3((unsigned)p.f.groups), dim3(256), 0, st, c);
     }
     if (p.many) {
-        const dim3 grid = set_plan(c, p.m, (char *)workspace + p.f_bytes, batch->batch);
+        set_workspace(c, (char *)workspace + p.f_bytes, p.m.units, p.m.units * p.m.splits, p.m.tile_rows);
+        c.row_tiles = p.m.row_tiles; c.splits = p.m.splits; c.split_tiles = p.m.split_tiles;
+        const dim3 grid((unsigned)((long)p.m.row_tiles * p.m.splits * c.a.n_kv), (unsigned)batch->batch);
         with_cache(cache, [&](auto ct, auto hd) {
             using CT = decltype(ct);
             if constexpr (sizeof(CT) != 4) {

@@ -28,11 +28,22 @@ struct PagedSeq {
 };
 __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs &a, int b) {
     PagedSeq s;
+    // (b is the workgroup's: the readfirstlanes say so, which keeps what follows from these in scalar registers)
+    s.row0 = min(max(__builtin_amdgcn_readfirstlane(a.q_starts[b]), 0), a.rows);
+    s.n_rows = min(max(__builtin_amdgcn_readfirstlane(a.q_starts[b + 1]), s.row0), a.rows) - s.row0;
+    s.kv = min(max(__builtin_amdgcn_readfirstlane(a.kv_lens[b]), 0), (int)min((long)a.table_width << a.page_shift, (long)0x7FFFFF00));
+    s.first = s.kv - s.n_rows;
+    s.table = a.table + (size_t)b * a.table_stride;
+    return s;
+}
+// the same for a number that differs from lane to lane
+__device__ __forceinline__ PagedSeq paged_seq_lane(const PagedArgs &a, int b) {
+    PagedSeq s;
     s.row0 = min(max(a.q_starts[b], 0), a.rows);
     s.n_rows = min(max(a.q_starts[b + 1], s.row0), a.rows) - s.row0;
     s.kv = min(max(a.kv_lens[b], 0), (int)min((long)a.table_width << a.page_shift, (long)0x7FFFFF00));
     s.first = s.kv - s.n_rows;
-    s.table = a.table + (size_t)b * a.table_stride;
+    s.table = nullptr;
     return s;
 }
 // The page of a position 0 <= pos < kv; -1: a hole
@@ -217,10 +228,11 @@ struct PagedAttn {
     int window, sinks;
     int once;                       // every key is read by one workgroup: requests are non-temporal (request_tile)
     int few_rows;                   // sequences with at most this many rows per KV head are k_paged_attn's, the others k_paged_chunk's
-    int row_tiles, splits, split_tiles;   // grid.x = row_tiles * splits * n_kv; at least split_tiles key tiles to a split
-    float *part_o;                  // [unit][split][tile row][head_dim], relative to the split's maximum
-    float2 *part_ml;                // [unit][split][tile row]: maximum (in bits), sum
-    int *tickets;                   // [unit], zero between launches
+    int row_tiles, splits, split_tiles;   // k_paged_chunk: grid.x = row_tiles * splits * n_kv; at least split_tiles key tiles to a split
+    int pairs, shares, min_share;   // k_paged_attn: (sequence, tile of rows) pairs, 0: a workgroup to a unit; grid.x; fewest groups of tiles to a workgroup
+    float *part_o;                  // [part][tile row][head_dim], relative to the part's maximum
+    float2 *part_ml;                // [part][tile row]: maximum (in bits), sum
+    int *tickets;                   // [(sequence, KV head, tile of rows)], zero between launches
 };
 
 constexpr int kKeyTile = 32;
@@ -281,6 +293,10 @@ __device__ __forceinline__ void request_words(const void *p, uint32_t lds) {
 // 16 bytes per lane likewise, to lds + 16 lane
 __device__ __forceinline__ void request_pieces(const void *p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+// a value that is the same in every lane, kept in scalar registers
+__device__ __forceinline__ size_t scalar(size_t v) {
+    return (size_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v) | (size_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
 }
 template <int N> __device__ __forceinline__ void wait_requests() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -375,7 +391,8 @@ struct PagedWave {
     template <bool ONCE>
     __device__ __forceinline__ void request(const PagedAttn &c, int base, int page0, int page1, int h, int lane, uint32_t to) const {
         const int mask = (1 << c.a.page_shift) - 1;
-        const size_t vec0 = paged_vec(c.a, max(page0, 0), h, base & mask), vec1 = paged_vec(c.a, max(page1, 0), h, (base + 16) & mask);
+        const size_t vec0 = scalar(paged_vec(c.a, max(page0, 0), h, base & mask)), vec1 = scalar(paged_vec(c.a, max(page1, 0), h, (base + 16) & mask));
+        to = __builtin_amdgcn_readfirstlane(to);
         if constexpr (kShort) {
             const size_t at = (lane < 32 ? vec0 : vec1) * kRow + from[0];
             request_pieces((const char *)c.a.k + at, to);
@@ -583,17 +600,29 @@ struct PagedWave {
     }
 };
 
-template <typename T> __device__ __forceinline__ void put_out(const PagedAttn &c, size_t at, float v);
-template <> __device__ __forceinline__ void put_out<float>(const PagedAttn &c, size_t at, float v) { ((float *)c.out.p)[at] = v; }
-template <> __device__ __forceinline__ void put_out<bf16_t>(const PagedAttn &c, size_t at, float v) { ((bf16_t *)c.out.p)[at].u = (uint16_t)pack_bf16(v, 0.f); }
-
-// Output d of a tile's row from its maximum, sum and weighted values; with d = 0 its log-sum-exp
+// Outputs d .. d + 3 of a tile's row from its maximum, sum and weighted values; with d = 0 its log-sum-exp
 template <typename OT>
-__device__ __forceinline__ void paged_finish(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int row, int d, float M, float L, float v) {
+__device__ __forceinline__ void paged_finish(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int row, int d, float M, float L, f32x4e_t v) {
     const int r = t.r0 + row, tok = r / c.group, qh = h * c.group + r % c.group;
-    put_out<OT>(c, (size_t)(s.row0 + tok) * c.out.row_stride + (size_t)qh * c.out.head_stride + d, L == 0.f ? 0.f : v / L);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    if (L == 0.f) v = f32x4e_t{0.f, 0.f, 0.f, 0.f};
+    v *= inv;
+    OT *p = (OT *)c.out.p + (size_t)(s.row0 + tok) * c.out.row_stride + (size_t)qh * c.out.head_stride + d;
+    if (c.out.vec) {
+        if constexpr (sizeof(OT) == 4) *(f32x4e_t *)p = v;
+        else *(u32x2_t *)p = u32x2_t{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(OT) == 4) p[i] = v[i];
+            else p[i].u = (uint16_t)pack_bf16(v[i], 0.f);
+        }
+    }
     if (c.lse && d == 0) c.lse[(size_t)(s.row0 + tok) * c.n_heads + qh] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994531f;
 }
+
+// 16 bytes written through to memory, as st_coherent (wait_stores before they are signalled)
+__device__ __forceinline__ void st_coherent4(float *p, f32x4e_t v) { asm volatile("global_store_dwordx4 %0, %1, off sc1" ::"v"(p), "v"(v) : "memory"); }
 
 // Whether this workgroup is the last of a unit's `used` to have written its part (its stores were st_coherent); leaves the ticket at zero
 __device__ __forceinline__ bool paged_last(const PagedAttn &c, size_t unit, int used, int *shared) {
@@ -608,149 +637,286 @@ __device__ __forceinline__ bool paged_last(const PagedAttn &c, size_t unit, int 
     return true;
 }
 
-// The parts of a unit joined: their order is that of the key ranges, whoever arrived last.  `table`: LDS for used * t.rows maxima and sums.
-template <typename OT, int HD>
-__device__ __forceinline__ void paged_join(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, size_t unit, int used, int tile_rows, float2 *table) {
-    const float2 *pm = c.part_ml + unit * c.splits * tile_rows;
-    for (int e = (int)threadIdx.x; e < used * t.rows; e += 256) table[e] = pm[(size_t)(e / t.rows) * tile_rows + e % t.rows];
-    __syncthreads();
-    for (int e = (int)threadIdx.x; e < t.rows * (HD / 4); e += 256) {
-        const int row = e / (HD / 4), d = e % (HD / 4) * 4;
-        const float *po = c.part_o + (unit * c.splits * tile_rows + row) * HD + d;
-        float M = -INFINITY, L = 0.f;
-        f32x4e_t v = {0.f, 0.f, 0.f, 0.f};
+// The parts of a unit joined, part i of `used` at place_of(i): their order is that of the key ranges, whoever arrived last.
+// A part is tile_rows * HD / 4 vectors of four outputs, of which the first `items` are looked at; where(e) says which row and outputs vector e is.  `table`: LDS for used * tile_rows maxima and
+// sums.  A thread has FLIGHT vectors on their way at a time, P parts of FLIGHT / P of its own (the last part again where there are fewer than P): this
+// is one workgroup's work while others may be done, and latency is what it costs.
+struct PagedWhere { int row, d; };
+template <typename OT, int HD, int P, int FLIGHT, typename F, typename G>
+__device__ __forceinline__ void paged_join_by(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int used, int items, size_t part_vecs, const float2 *table, F place_of, G where) {
+    constexpr int kItems = FLIGHT / P;
+    for (int e0 = (int)threadIdx.x; e0 < items; e0 += 256 * kItems) {
+        float M[kItems], L[kItems];
+        f32x4e_t v[kItems];
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) {
+            const int row = min(where(min(e0 + 256 * k, items - 1)).row, t.rows - 1);
+            M[k] = -INFINITY; L[k] = 0.f;
+            v[k] = f32x4e_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-        for (int i = 0; i < used; ++i) M = fmaxf(M, table[i * t.rows + row].x);
-        const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll 16
-        for (int i = 0; i < used; ++i) {
-            const float2 x = table[i * t.rows + row];
-            const float f = __builtin_amdgcn_exp2f(x.x - ref);
-            L += f * x.y;
-            v += f * *(const f32x4e_t *)(po + (size_t)i * tile_rows * HD);
+            for (int i = 0; i < used; ++i) M[k] = fmaxf(M[k], table[i * t.rows + row].x);
+        }
+        for (int i0 = 0; i0 < used; i0 += P) {
+            f32x4e_t x[kItems][P];
+#pragma unroll
+            for (int k = 0; k < kItems; ++k)
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    x[k][i] = f32x4e_t{0.f, 0.f, 0.f, 0.f};
+                    if (where(min(e0 + 256 * k, items - 1)).row < t.rows)        // the others were not written
+                        x[k][i] = ((gptr<f32x4e_t>)c.part_o)[(size_t)place_of(min(i0 + i, used - 1)) * part_vecs + min(e0 + 256 * k, items - 1)];
+                }
+#pragma unroll
+            for (int k = 0; k < kItems; ++k) {
+                const int row = min(where(min(e0 + 256 * k, items - 1)).row, t.rows - 1);
+                const float ref = M[k] == -INFINITY ? 0.f : M[k];
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const float2 y = table[min(i0 + i, used - 1) * t.rows + row];
+                    const float f = i0 + i < used ? __builtin_amdgcn_exp2f(y.x - ref) : 0.f;
+                    L[k] += f * y.y;
+                    v[k] += f * x[k][i];
+                }
+            }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) paged_finish<OT>(c, s, t, h, row, d + i, M, L, v[i]);
+        for (int k = 0; k < kItems; ++k) {
+            const int e = e0 + 256 * k;
+            const PagedWhere w = where(min(e, items - 1));
+            if (e < items && w.row < t.rows) paged_finish<OT>(c, s, t, h, w.row, w.d, M[k], L[k], v[k]);
+        }
     }
 }
+template <typename OT, int HD, int FLIGHT, typename F, typename G>
+__device__ __forceinline__ void paged_join(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int used, int tile_rows, int items, float2 *table, F place_of, G where) {
+    const size_t part_vecs = (size_t)tile_rows * (HD / 4);
+    for (int e = (int)threadIdx.x; e < used * t.rows; e += 256) table[e] = c.part_ml[(size_t)place_of(e / t.rows) * tile_rows + e % t.rows];
+    __syncthreads();
+    if (used <= 4) paged_join_by<OT, HD, 4, FLIGHT>(c, s, t, h, used, items, part_vecs, table, place_of, where);
+    else if (used <= 8) paged_join_by<OT, HD, 8, FLIGHT>(c, s, t, h, used, items, part_vecs, table, place_of, where);
+    else paged_join_by<OT, HD, FLIGHT, FLIGHT>(c, s, t, h, used, items, part_vecs, table, place_of, where);
+}
 
-// Attention of few rows per KV head, and of float32 models' rows however many: a workgroup takes NB blocks of 16 rows of one
-// KV head and a range of keys, its four waves every fourth tile of the range.  The waves' results are joined through LDS, the ranges' by the
-// workgroup that arrives last.
+// Sum over the lanes up to this one, by moves between lanes (DPP: within rows of 16, then row to row)
+__device__ __forceinline__ int sum_to_lane(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // row_bcast:15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);      // row_bcast:31 into rows 2 and 3
+    return v;
+}
+
+// A unit is a KV head of a (sequence, tile of rows) pair; its work is counted in groups of kGroup key tiles, one tile to each of a workgroup's waves.
+constexpr int kGroup = 4;
+struct PagedUnit {
+    int pair, h;
+    int first, groups;              // number of its first group among all units', how many it has
+};
+
+// Attention of few rows per KV head, and of float32 models' rows however many.
+//  The groups of all units, in the order (pair, KV head), are cut into equal shares, a share to a workgroup: sequences of all lengths keep
+//  every compute unit busy to the end, whatever the host knows of the lengths (each wave adds up the pairs' groups itself, 64 at a time).
+//  A share is some whole units and up to two parts of units; a part's result goes to memory and the unit's last workgroup to arrive joins them.
+//  Where there are more pairs than a wave adds up in a reasonable time, a workgroup takes a unit (c.pairs = 0).
+//  A workgroup has NB blocks of 16 rows and all four waves work on the same ones, each on every fourth key tile; they are joined through LDS.
 template <typename CT, int HD, int NB>
 __global__ __launch_bounds__(256, (NB * HD < 256 && sizeof(CT) < 4) || HD == 32 ? 2 : 1) void k_paged_attn(PagedAttn c) {
     using W = PagedWave<CT, HD, NB>;
     using OT = typename std::conditional<sizeof(CT) == 4, float, bf16_t>::type;
-    constexpr int kWaveBytes = W::kRing * W::kTile, kJoin = 4 * 16 * (HD + 4) * 4;
-    constexpr int kTable = kPagedMaxSplits * NB * 16 * 8;
-    constexpr int kBytes = 4 * kWaveBytes > kJoin ? (4 * kWaveBytes > kTable ? 4 * kWaveBytes : kTable) : (kJoin > kTable ? kJoin : kTable);
+    constexpr int kRows = NB * 16, kWaveBytes = W::kRing * W::kTile, kJoin = 4 * 16 * (HD + 4) * 4;
+    constexpr int kBytes = 4 * kWaveBytes > kJoin ? 4 * kWaveBytes : kJoin;
     __shared__ __align__(1024) char lds[kBytes];
-    __shared__ float2 ml[4][NB * 16];
+    __shared__ float2 ml[4][kRows];
     __shared__ int last_one;
     float (*ob)[16][HD + 4] = (float (*)[16][HD + 4])lds;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int h = (int)blockIdx.x % c.a.n_kv, rest = (int)blockIdx.x / c.a.n_kv;
-    const int split = rest % c.splits, tile = c.row_tiles - 1 - rest / c.splits;    // later rows see more: they start first
-    const PagedSeq s = paged_seq(c.a, blockIdx.y);
-    if (s.n_rows * c.group > c.few_rows) return;                         // k_paged_chunk's
-    const PagedTile t = paged_tile<kKeyTile>(c, s, tile, NB * 16);
-    if (t.rows == 0) return;
-    const int per = max(c.split_tiles, (t.tiles + c.splits - 1) / c.splits), used = max(1, (t.tiles + per - 1) / per);
-    if (split >= used) return;
-    const int begin = split * per, end = min(begin + per, t.tiles);
+    const int n = lane & 15, g = lane >> 4;
 
-    W w;
-    w.init(c, s, t, h, lane);
-    // This wave's tiles are begin + wave + 4 i, i < count.  Pages are looked up 32 tiles at a time: lane 2 i + half.
-    const int count = end - begin > wave ? (end - begin - wave + 3) / 4 : 0;
-    auto key_base = [&](int i) { const int v = begin + wave + 4 * i; return (v < t.n_sink ? v : v - t.n_sink + t.t_lo) * kKeyTile; };
-    auto look_up = [&](int i0) {
-        const int i = i0 + (lane >> 1);
-        if (i >= count) return -1;
-        const int pos = key_base(i) + 16 * (lane & 1);
-        return pos < s.kv ? paged_page(c.a, s, pos) : -1;
+    // ---- which groups are this workgroup's.  The first 64 pairs stay in registers, lane by lane.
+    auto pair_of = [&](int pair, PagedSeq &s) {  // a pair's groups of one KV head; at least 1 where there are rows, since they have to be written
+        if (pair >= c.pairs && c.pairs) return 0;
+        s = paged_seq_lane(c.a, c.row_tiles == 1 ? pair : pair / c.row_tiles);
+        if (s.n_rows * c.group > c.few_rows) return 0;                   // k_paged_chunk's
+        const PagedTile t = paged_tile<kKeyTile>(c, s, c.row_tiles == 1 ? 0 : pair % c.row_tiles, kRows);
+        return t.rows == 0 ? 0 : max(1, (t.tiles + kGroup - 1) / kGroup);
     };
-    if (count > 0) {
+    int pos = 0, end = 0, share = 1;             // (the host sees to it that all groups fit 30 bits)
+    PagedSeq first64{};
+    int groups64 = 0, sum64 = 0;
+    auto locate = [&](int at, PagedUnit &u, PagedSeq &s) {
+        int before = 0;
+        for (int p0 = 0; p0 < c.pairs; p0 += kWave) {
+            PagedSeq x = first64;
+            const int mine = p0 ? pair_of(p0 + lane, x) : groups64, sum = p0 ? sum_to_lane(mine) : sum64;
+            const int first = (before + sum - mine) * c.a.n_kv;
+            const uint64_t hit = __ballot(mine > 0 && first <= at && at < first + mine * c.a.n_kv);
+            if (hit) {
+                const int i = __builtin_ctzll(hit);
+                u.pair = p0 + i;
+                u.groups = __builtin_amdgcn_readlane(mine, i);
+                u.first = __builtin_amdgcn_readlane(first, i);
+                u.h = (at - u.first) / u.groups;
+                u.first += u.h * u.groups;
+                s.row0 = __builtin_amdgcn_readlane(x.row0, i);
+                s.n_rows = __builtin_amdgcn_readlane(x.n_rows, i);
+                s.kv = __builtin_amdgcn_readlane(x.kv, i);
+                s.first = s.kv - s.n_rows;
+                s.table = c.a.table + (size_t)(u.pair / c.row_tiles) * c.a.table_stride;
+                return true;
+            }
+            before += __builtin_amdgcn_readlane(sum, kWave - 1);
+        }
+        return false;                            // not while the lengths stay what they were when the groups were counted
+    };
+    PagedUnit u{};
+    PagedSeq s;
+    if (c.pairs) {
+        groups64 = pair_of(lane, first64);
+        sum64 = sum_to_lane(groups64);
+        int total = __builtin_amdgcn_readlane(sum64, kWave - 1), most = groups64;
+        for (int p0 = kWave; p0 < c.pairs; p0 += kWave) {
+            PagedSeq x;
+            const int mine = pair_of(p0 + lane, x);
+            most = max(most, mine);
+            total += __builtin_amdgcn_readlane(sum_to_lane(mine), kWave - 1);
+        }
+        total *= c.a.n_kv;
+        // equal shares, none smaller than is worth a workgroup, and none so small that LDS could not hold the maxima and sums of a unit's parts
+        constexpr int kParts = kBytes / (kRows * 8) - 2;
+        share = max(c.min_share, (int)((unsigned)(total + c.shares - 1) / (unsigned)c.shares));
+        if (total / c.a.n_kv > share * kParts) {
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, kWave));
+            share = max(share, __builtin_amdgcn_readfirstlane(most) / kParts + 1);
+        }
+        pos = share * (int)blockIdx.x;
+        end = min(pos + share, total);
+        if (pos >= end || !locate(pos, u, s)) return;
+    } else {
+        u.pair = (int)blockIdx.x / c.a.n_kv;
+        u.h = (int)blockIdx.x % c.a.n_kv;
+        PagedSeq x;
+        u.groups = end = __builtin_amdgcn_readfirstlane(pair_of(u.pair, x));
+        if (end == 0) return;
+        s = paged_seq(c.a, u.pair / c.row_tiles);
+    }
+
+    for (;;) {
+        const int h = u.h, pair = u.pair;
+        const PagedTile t = paged_tile<kKeyTile>(c, s, pair % c.row_tiles, kRows);
+        // groups g0 .. g1 of the unit; the whole of it, or one of `used` parts
+        const int g0 = pos - u.first, g1 = min(end, u.first + u.groups) - u.first;
+        const bool part = g1 - g0 < u.groups;
+        const int begin = g0 * kGroup, stop = min(g1 * kGroup, t.tiles);
+
+        // This wave's tiles are begin + wave + 4 i, i < count.  Pages are looked up 32 tiles at a time: lane 2 i + half.
+        const int count = stop - begin > wave ? (stop - begin - wave + 3) / 4 : 0;
+        auto key_base = [&](int i) { const int v = begin + wave + 4 * i; return (v < t.n_sink ? v : v - t.n_sink + t.t_lo) * kKeyTile; };
+        auto look_up = [&](int i0) {
+            const int i = i0 + (lane >> 1);
+            if (i >= count) return -1;
+            const int at = key_base(i) + 16 * (lane & 1);
+            return at < s.kv ? paged_page(c.a, s, at) : -1;
+        };
         // pages of the tiles being requested, of the next 32, and of the 32 that are worked on
         int pages = look_up(0), pages_next = count > 32 ? look_up(32) : -1, pages_old = pages;
-        const uint32_t ring = lds_address(lds) + wave * kWaveBytes;
-        auto request = [&](int i) {
-            if ((i & 31) == 0 && i) {
-                pages_old = pages;
-                pages = pages_next;
-                pages_next = i + 32 < count ? look_up(i + 32) : -1;
-            }
-            const int p0 = __builtin_amdgcn_readlane(pages, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + 1);
-            const uint32_t to = ring + (i % W::kRing) * W::kTile;
-            if (c.once) w.template request<true>(c, key_base(i), p0, p1, h, lane, to);
-            else w.template request<false>(c, key_base(i), p0, p1, h, lane, to);
-        };
+        W w;
+        w.init(c, s, t, h, lane);
+        if (count > 0) {
+            const uint32_t ring = lds_address(lds) + wave * kWaveBytes;
+            auto request = [&](int i) {
+                if ((i & 31) == 0 && i) {
+                    pages_old = pages;
+                    pages = pages_next;
+                    pages_next = i + 32 < count ? look_up(i + 32) : -1;
+                }
+                const int p0 = __builtin_amdgcn_readlane(pages, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + 1);
+                const uint32_t to = ring + (i % W::kRing) * W::kTile;
+                if (c.once) w.template request<true>(c, key_base(i), p0, p1, h, lane, to);
+                else w.template request<false>(c, key_base(i), p0, p1, h, lane, to);
+            };
 #pragma unroll
-        for (int i = 0; i < W::kRing; ++i)
-            if (i < count) request(i);
-        int asked = min(count, W::kRing);
-        for (int i = 0; i < count; ++i) {
-            // of the tiles asked for, all but this one may still be on their way
-            if (asked - i >= W::kRing) wait_requests<(W::kRing - 1) * W::kRequests>();
-            else wait_requests<0>();
-            const int base = key_base(i), from = (asked - 1) >> 5 == i >> 5 ? pages : pages_old;
-            const int p0 = __builtin_amdgcn_readlane(from, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(from, 2 * (i & 31) + 1);
-            const uint32_t at = ring + (i % W::kRing) * W::kTile;
-            if (W::whole(c, t, base, p0, p1)) w.template take<false>(c, s, t, h, lane, base, p0, p1, at);
-            else w.template take<true>(c, s, t, h, lane, base, p0, p1, at);
-            if (asked < count) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // what was read of the tile is here: its place is free
-                request(asked++);
+            for (int i = 0; i < W::kRing; ++i)
+                if (i < count) request(i);
+            int asked = min(count, W::kRing);
+            for (int i = 0; i < count; ++i) {
+                // of the tiles asked for, all but this one may still be on their way
+                if (asked - i >= W::kRing) wait_requests<(W::kRing - 1) * W::kRequests>();
+                else wait_requests<0>();
+                const int base = key_base(i), from = (asked - 1) >> 5 == i >> 5 ? pages : pages_old;
+                const int p0 = __builtin_amdgcn_readlane(from, 2 * (i & 31)), p1 = __builtin_amdgcn_readlane(from, 2 * (i & 31) + 1);
+                const uint32_t at = ring + (i % W::kRing) * W::kTile;
+                if (W::whole(c, t, base, p0, p1)) w.template take<false>(c, s, t, h, lane, base, p0, p1, at);
+                else w.template take<true>(c, s, t, h, lane, base, p0, p1, at);
+                if (asked < count) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // what was read of the tile is here: its place is free
+                    request(asked++);
+                }
             }
         }
-    }
 
-    const int n = lane & 15, g = lane >> 4;
+        // ---- the four waves' results
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        w.l[b] += __shfl_xor(w.l[b], 16, kWave);
-        w.l[b] += __shfl_xor(w.l[b], 32, kWave);
-        if (w.l[b] != w.l[b] && w.m[b] == -INFINITY) w.m[b] = 0.f;      // nothing but NaN: a NaN, not an empty row
-        if (g == 0) ml[wave][b * 16 + n] = make_float2(w.m[b], w.l[b]);
-    }
-    __syncthreads();
-    const size_t unit = ((size_t)blockIdx.y * c.a.n_kv + h) * c.row_tiles + tile;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        float M = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) M = fmaxf(M, ml[i][b * 16 + n].x);
-        const float f = w.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m[b] - M);
-        if (b) __syncthreads();
-#pragma unroll
-        for (int i = 0; i < HD / 16; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) ob[wave][n][W::dim_of(i, r, g)] = w.m[b] == -INFINITY ? 0.f : w.o[b][i][r] * f;
+        for (int b = 0; b < NB; ++b) {
+            w.l[b] += __shfl_xor(w.l[b], 16, kWave);
+            w.l[b] += __shfl_xor(w.l[b], 32, kWave);
+            if (w.l[b] != w.l[b] && w.m[b] == -INFINITY) w.m[b] = 0.f;      // nothing but NaN: a NaN, not an empty row
+            if (g == 0) ml[wave][b * 16 + n] = make_float2(w.m[b], w.l[b]);
+        }
         __syncthreads();
-        const int row = (int)threadIdx.x >> 4;
-        if (b * 16 + row < t.rows) {
-            float R = -INFINITY, L = 0.f;
+        // a part's place: 2 to a workgroup, the first for the unit that its share begins with
+        const size_t place = 2 * (size_t)blockIdx.x + (pos == share * blockIdx.x ? 0 : 1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) R = fmaxf(R, ml[i][b * 16 + row].x);
+        for (int b = 0; b < NB; ++b) {
+            float M = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { const float2 e = ml[i][b * 16 + row]; L += e.x == -INFINITY ? 0.f : e.y * __builtin_amdgcn_exp2f(e.x - R); }
+            for (int i = 0; i < 4; ++i) M = fmaxf(M, ml[i][b * 16 + n].x);
+            const float f = w.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m[b] - M);
+            if (b) __syncthreads();
 #pragma unroll
-            for (int i = 0; i < HD / 16; ++i) {
-                const int d = i * 16 + ((int)threadIdx.x & 15);
-                const float v = ob[0][row][d] + ob[1][row][d] + ob[2][row][d] + ob[3][row][d];
-                if (used == 1) paged_finish<OT>(c, s, t, h, b * 16 + row, d, R, L, v);
-                else st_coherent(c.part_o + ((unit * c.splits + split) * (NB * 16) + b * 16 + row) * HD + d, v);
-            }
-            if (used > 1 && ((int)threadIdx.x & 15) == 0) {
-                float *p = (float *)(c.part_ml + (unit * c.splits + split) * (NB * 16) + b * 16 + row);
-                st_coherent(p, R);
-                st_coherent(p + 1, L);
+            for (int i = 0; i < HD / 16; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) ob[wave][n][W::dim_of(i, r, g)] = w.m[b] == -INFINITY ? 0.f : w.o[b][i][r] * f;
+            __syncthreads();
+            for (int e = (int)threadIdx.x; e < 16 * (HD / 4); e += 256) {
+                const int row = e / (HD / 4), d = e % (HD / 4) * 4;
+                if (b * 16 + row >= t.rows) break;
+                float R = -INFINITY, L = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) R = fmaxf(R, ml[i][b * 16 + row].x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { const float2 e = ml[i][b * 16 + row]; L += e.x == -INFINITY ? 0.f : e.y * __builtin_amdgcn_exp2f(e.x - R); }
+                f32x4e_t v = *(const f32x4e_t *)&ob[0][row][d];
+#pragma unroll
+                for (int i = 1; i < 4; ++i) v += *(const f32x4e_t *)&ob[i][row][d];
+                if (!part) {
+                    paged_finish<OT>(c, s, t, h, b * 16 + row, d, R, L, v);
+                } else {
+                    st_coherent4(c.part_o + (place * kRows + b * 16 + row) * HD + d, v);
+                    if (d == 0) {
+                        float *p = (float *)(c.part_ml + place * kRows + b * 16 + row);
+                        st_coherent(p, R);
+                        st_coherent(p + 1, L);
+                    }
+                }
             }
         }
+        if (part) {
+            const int w0 = u.first / share, used = (u.first + u.groups - 1) / share - w0 + 1;
+            if (paged_last(c, ((size_t)(pair / c.row_tiles) * c.a.n_kv + h) * c.row_tiles + pair % c.row_tiles, used, &last_one)) {
+                const int skew = u.first == w0 * share ? 0 : 1;
+                paged_join<OT, HD, 32>(c, s, t, h, used, kRows, t.rows * (HD / 4), (float2 *)lds, [&](int i) { return 2 * (w0 + i) + (i == 0 ? skew : 0); },
+                                         [](int e) { return PagedWhere{e / (HD / 4), e % (HD / 4) * 4}; });
+            }
+        }
+        pos = u.first + g1;
+        if (pos >= end) return;
+        __syncthreads();
+        if (++u.h < c.a.n_kv) u.first += u.groups;
+        else if (!locate(pos, u, s)) return;
     }
-    if (used == 1) return;
-    if (!paged_last(c, unit, used, &last_one)) return;
-    paged_join<OT, HD>(c, s, t, h, unit, used, NB * 16, (float2 *)lds);
 }
 
 }  // namespace ead

@@ -305,21 +305,23 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
         if (c.lse && hh == 0) c.lse[(size_t)(s.row0 + my_tok) * c.n_heads + my_head] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
         return;
     }
-    const size_t slot = (unit * c.splits + split) * kChunkRows;
+    // a part's vectors in the order [wave][x][e][lane]: neighbouring lanes write neighbouring bytes
+    const size_t slot = unit * c.splits + split;
     if (n < w_rows) {
-        float *p = c.part_o + (slot + 32 * wave + n) * HD;
+        float *p = c.part_o + (slot * kChunkRows * HD / 4 + (size_t)wave * CB * 256 + lane) * 4;
 #pragma unroll
         for (int x = 0; x < CB; ++x)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) st_coherent(p + 32 * x + 8 * (e >> 2) + 4 * hh + (e & 3), o[x][e]);
+            for (int e = 0; e < 4; ++e) st_coherent4(p + (x * 4 + e) * 256, f32x4e_t{o[x][4 * e], o[x][4 * e + 1], o[x][4 * e + 2], o[x][4 * e + 3]});
         if (hh == 0) {
-            float *pm = (float *)(c.part_ml + slot + 32 * wave + n);
+            float *pm = (float *)(c.part_ml + slot * kChunkRows + 32 * wave + n);
             st_coherent(pm, m);
             st_coherent(pm + 1, l);
         }
     }
     if (!paged_last(c, unit, used, &last_one)) return;
-    paged_join<bf16_t, HD>(c, s, t, h, unit, used, kChunkRows, (float2 *)lds);
+    paged_join<bf16_t, HD, 16>(c, s, t, h, used, kChunkRows, kChunkRows * (HD / 4), (float2 *)lds, [&](int i) { return unit * c.splits + i; },
+                               [](int e) { return PagedWhere{e / (CB * 256) * 32 + (e & 31), e / 256 % CB * 32 + e / 64 % 4 * 8 + (e & 32) / 8}; });
 }
 
 }  // namespace ead

@@ -4,13 +4,12 @@
 
 namespace ead {
 
-constexpr int kPagedMaxSplits = 64;
 
-// Blocks of 16 rows that a wave's registers hold at most: float queries and outputs of 128 dimensions take twice as many
-constexpr int paged_max_blocks(bool f32, int head_dim) { return f32 && head_dim == 128 ? 2 : 4; }
+// Blocks of 16 rows that a wave's registers hold at most
+constexpr int paged_max_blocks(int head_dim) { return head_dim == 128 ? 2 : 4; }
 
 // Rows per KV head (new tokens times query heads per KV head) of a sequence up to which k_paged_attn takes it
-constexpr int kPagedFewRows = 64;
+constexpr int paged_few_rows(int head_dim) { return head_dim == 128 ? 32 : 64; }
 
 // Keys a row sees at most up to which k_paged_chunk takes two bf16 terms of every probability (its comment has both sides)
 constexpr int kPagedTwoTerms = 4096;
@@ -44,23 +43,46 @@ inline PagedPlan paged_cut(int tile_rows, int key_tile, long rows, int batch, in
     return p;
 }
 
-// k_paged_attn: ranges of keys where there are too few tiles of rows for four workgroups a compute unit, none shorter than a tile for each
-// of a workgroup's four waves
-inline PagedPlan paged_few(int batch, int n_kv, int group, long rows, int max_kv, int window, int sinks, int cus, int nb_max) {
-    const int nb = rows <= 16 ? 1 : rows <= 32 ? 2 : nb_max;
-    return paged_cut(16 * nb, 32, rows, batch, n_kv, group, max_kv, window, sinks, 4l * cus, 4, kPagedMaxSplits);
+// A launch of k_paged_attn: blocks of 16 rows to a workgroup, tiles of rows per KV head, pairs it cuts into shares (0: a workgroup to a unit),
+// workgroups, and the parts of units that there may be
+struct PagedShares {
+    int nb, row_tiles, pairs, min_share;
+    long units, groups, parts;
+};
+constexpr long kPagedMaxPairs = 1024;      // pairs a wave adds up before it starts; with more there are enough units for every compute unit
+// Groups (128 keys) a workgroup starts for at least
+constexpr int kPagedMinShare = 2;
+// Units of up to this many groups go to a workgroup each: cutting them saves less time than adding up the shares and joining the parts takes
+// (16 sequences of 1000 8-bit keys: 19 us whole, 27 in shares; of 8000: 103 and 57)
+constexpr long kPagedWholeGroups = 8;
+
+// `capacity`: positions a row of the page table reaches, whatever max_kv says; `resident`: workgroups of the kernel the device holds at once
+inline PagedShares paged_few(int batch, int n_kv, long rows, int nb, int group, int max_kv, long capacity, int window, int sinks, long resident) {
+    PagedShares p;
+    p.nb = nb;
+    p.row_tiles = (int)std::max(1l, (rows + 16 * nb - 1) / (16 * nb));
+    const long pairs = (long)batch * p.row_tiles;
+    p.units = pairs * n_kv;
+    const long each = (paged_keys(16 * nb, 32, group, max_kv, window, sinks) + 127) / 128;
+    const bool whole = each <= kPagedWholeGroups || (p.row_tiles > 1 && p.units >= resident);
+    p.pairs = !whole && pairs <= kPagedMaxPairs && p.units * ((capacity + 127) / 128) < 1l << 30 ? (int)pairs : 0;
+    p.min_share = kPagedMinShare;
+    p.groups = p.pairs ? std::max(1l, std::min(resident, (p.units * each + p.min_share - 1) / p.min_share)) : p.units;
+    p.parts = p.pairs ? 2 * p.groups : 0;
+    return p;
+}
+inline int paged_blocks(long rows, int nb_max) { return rows <= 16 ? 1 : rows <= 32 ? 2 : nb_max; }
+
+// Workspace of a launch: a ticket per unit (to a multiple of 64), then every part's maxima and sums, then its outputs
+inline unsigned long long paged_workspace(long units, long parts, int tile_rows, int head_dim) {
+    if (parts == 0) return 0;
+    const unsigned long long rows = (unsigned long long)parts * tile_rows;
+    return ((unsigned long long)units + 63) / 64 * 256 + rows * 8 + rows * head_dim * 4;
 }
 
 // k_paged_chunk: two workgroups fit a compute unit
 inline PagedPlan paged_many(int batch, int n_kv, int group, long rows, int max_kv, int window, int sinks, int cus, int head_dim) {
     return paged_cut(128, 64, rows, batch, n_kv, group, max_kv, window, sinks, 2l * cus, 4, paged_many_splits(head_dim));
-}
-
-// Workspace of a launch: a ticket per unit (to a multiple of 64), then every range's maxima and sums, then its outputs
-inline unsigned long long paged_bytes(const PagedPlan &p, int head_dim) {
-    if (p.splits == 1) return 0;
-    const unsigned long long rows = (unsigned long long)p.units * p.splits * p.tile_rows;
-    return ((unsigned long long)p.units + 63) / 64 * 256 + rows * 8 + rows * head_dim * 4;
 }
 
 }  // namespace ead
