@@ -165,6 +165,7 @@ FewKernel few_kernel(const ead_paged_cache *c, int nb) {
 // The launches of a call: sequences with few rows (of a float32 cache: all), then those with many
 struct PagedCall {
     bool few, many, two;
+    int few_rows;
     FewKernel kernel;
     PagedShares f;
     PagedPlan m;
@@ -175,11 +176,14 @@ PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_
     const bool f32 = c->dtype == EAD_F32;
     const long rows = (long)b->max_q * group;
     PagedCall p{};
-    p.few = f32 || (long)b->min_q * group <= paged_few_rows(c->head_dim);
-    p.many = !f32 && rows > paged_few_rows(c->head_dim);
+    const double work = paged_work(b->batch, c->n_kv_heads, c->head_dim, group, rows, held, at->window, at->sinks);
+    const double kv_bytes = 2.0 * b->batch * c->n_kv_heads * c->head_dim * element_bytes(c->dtype) * (double)paged_keys(16, 32, group, held, at->window, at->sinks);
+    p.few_rows = f32 || work <= kPagedSmallWork ? 0x7FFFFFFF : paged_few_rows(c->head_dim);
+    p.few = (long)b->min_q * group <= p.few_rows;
+    p.many = rows > p.few_rows;
     if (p.few) {
-        const long few = f32 ? rows : std::min(rows, (long)paged_few_rows(c->head_dim));
-        const int nb = paged_blocks(few, paged_max_blocks(c->head_dim));
+        const long few = std::min(rows, (long)p.few_rows);
+        const int nb = paged_blocks(f32, few, paged_max_blocks(c->head_dim), work, kv_bytes);
         p.kernel = few_kernel(c, nb);
         p.f = paged_few(b->batch, c->n_kv_heads, few, nb, group, held, (long)b->table_width * c->page_size, at->window, at->sinks, p.kernel.resident);
         p.f_bytes = paged_workspace(p.f.units, p.f.parts, 16 * nb, c->head_dim);
@@ -239,8 +243,7 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     c.c2 = attn->scale * 1.4426950408889634f;
     c.window = attn->window;
     c.sinks = attn->sinks;
-    const bool f32 = cache->dtype == EAD_F32;
-    c.few_rows = f32 ? 0x7FFFFFFF : paged_few_rows(cache->head_dim);
+    c.few_rows = p.few_rows;
     const hipStream_t st = (hipStream_t)hip_stream;
     if (p.few) {
         set_workspace(c, workspace, p.f.units, p.f.parts, 16 * p.f.nb);

@@ -53,8 +53,9 @@ constexpr long kPagedMaxPairs = 1024;      // pairs a wave adds up before it sta
 // Groups (128 keys) a workgroup starts for at least
 constexpr int kPagedMinShare = 2;
 // Units of up to this many groups go to a workgroup each: cutting them saves less time than adding up the shares and joining the parts takes
-// (16 sequences of 1000 8-bit keys: 19 us whole, 27 in shares; of 8000: 103 and 57)
-constexpr long kPagedWholeGroups = 8;
+// (16 sequences of 1000 8-bit keys: 18 us whole, 27 in shares; of 8000: 103 and 56).  Fewer units than kPagedManyUnits leave most of the device idle:
+// there up to half as many (one sequence of 1000 keys, 8 KV heads: 17 whole, 13 in shares).
+constexpr long kPagedWholeGroups = 8, kPagedManyUnits = 32;
 
 // `capacity`: positions a row of the page table reaches, whatever max_kv says; `resident`: workgroups of the kernel the device holds at once
 inline PagedShares paged_few(int batch, int n_kv, long rows, int nb, int group, int max_kv, long capacity, int window, int sinks, long resident) {
@@ -64,14 +65,31 @@ inline PagedShares paged_few(int batch, int n_kv, long rows, int nb, int group, 
     const long pairs = (long)batch * p.row_tiles;
     p.units = pairs * n_kv;
     const long each = (paged_keys(16 * nb, 32, group, max_kv, window, sinks) + 127) / 128;
-    const bool whole = each <= kPagedWholeGroups || (p.row_tiles > 1 && p.units >= resident);
+    const bool whole = each <= (p.units >= kPagedManyUnits ? kPagedWholeGroups : kPagedWholeGroups / 2) || (p.row_tiles > 1 && p.units >= resident);
     p.pairs = !whole && pairs <= kPagedMaxPairs && p.units * ((capacity + 127) / 128) < 1l << 30 ? (int)pairs : 0;
     p.min_share = kPagedMinShare;
     p.groups = p.pairs ? std::max(1l, std::min(resident, (p.units * each + p.min_share - 1) / p.min_share)) : p.units;
     p.parts = p.pairs ? 2 * p.groups : 0;
     return p;
 }
-inline int paged_blocks(long rows, int nb_max) { return rows <= 16 ? 1 : rows <= 32 ? 2 : nb_max; }
+
+// Operations of a call at the most
+inline double paged_work(int batch, int n_kv, int head_dim, int group, long rows, int max_kv, int window, int sinks) {
+    return 4.0 * head_dim * n_kv * rows * batch * (double)paged_keys(16, 32, group, max_kv, window, sinks);
+}
+// Calls of up to this much work are latency: k_paged_attn takes them alone, however many rows their sequences have (a second launch and k_paged_chunk's longer start
+// cost more than its products save; 32 heads, 64 rows after 1000 keys, 1.1e9: 24 us against 36; 256 rows after 2000, 9.4e9: 43 and 47; 8 prompts of 256,
+// 8.6e9: 92 and 24)
+constexpr double kPagedSmallWork = 4e9;
+// Blocks of 16 rows to a workgroup.  One where the work is small and K and V come from the second-level caches when other blocks read them again: more workgroups
+// share the work (8 sequences of 32 rows after 2000 keys 27 us with one block, 31 with two; 32 of them 71 and 52).  Float products take eight times
+// as long, and the measured bounds are lower (prompts of 3 x 500: 20 / 19 / 21 us with 1 / 2 / 4 blocks; 8 x 500 after 500: 67 / 57 / 51).
+inline int paged_blocks(bool f32, long rows, int nb_max, double work, double kv_bytes) {
+    if (rows <= 16) return 1;
+    if (work <= (f32 ? kPagedSmallWork / 8 : kPagedSmallWork) && kv_bytes <= 64e6) return 1;
+    if (rows <= 32 || (f32 && work <= kPagedSmallWork / 2)) return 2;
+    return nb_max;
+}
 
 // Workspace of a launch: a ticket per unit (to a multiple of 64), then every part's maxima and sums, then its outputs
 inline unsigned long long paged_workspace(long units, long parts, int tile_rows, int head_dim) {
