@@ -198,7 +198,7 @@ PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_
 
 void set_workspace(PagedAttn &c, void *ws, long units, long parts, int tile_rows) {
     c.tickets = (int *)ws;
-    c.part_ml = (float2 *)((char *)ws + (units + 63) / 64 * 256);
+    c.part_ml = (float2 *)((char *)ws + units * kPagedTicketInts * 4);
     c.part_o = (float *)(c.part_ml + (size_t)parts * tile_rows);
 }
 

@@ -232,7 +232,7 @@ struct PagedAttn {
     int pairs, shares, min_share;   // k_paged_attn: (sequence, tile of rows) pairs, 0: a workgroup to a unit; grid.x; fewest groups of tiles to a workgroup
     float *part_o;                  // [part][tile row][head_dim], relative to the part's maximum
     float2 *part_ml;                // [part][tile row]: maximum (in bits), sum
-    int *tickets;                   // [(sequence, KV head, tile of rows)], zero between launches
+    int *tickets;                   // [(sequence, KV head, tile of rows)] in cache lines of their own, zero between launches
 };
 
 constexpr int kKeyTile = 32;
@@ -624,16 +624,39 @@ __device__ __forceinline__ void paged_finish(const PagedAttn &c, const PagedSeq 
 // 16 bytes written through to memory, as st_coherent (wait_stores before they are signalled)
 __device__ __forceinline__ void st_coherent4(float *p, f32x4e_t v) { asm volatile("global_store_dwordx4 %0, %1, off sc1" ::"v"(p), "v"(v) : "memory"); }
 
+// What others wrote through, read past the caches that may hold something older
+__device__ __forceinline__ float2 ld_coherent2(const float2 *p) {
+    const unsigned long long v = __hip_atomic_load((const unsigned long long *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+__device__ __forceinline__ f32x4e_t ld_coherent4(const float *p) {
+    const float2 a = ld_coherent2((const float2 *)p), b = ld_coherent2((const float2 *)p + 1);
+    return f32x4e_t{a.x, a.y, b.x, b.y};
+}
+
+// How a join reads its parts: past the caches (PAST), 8 bytes at a time, or by plain loads after an acquire of the device's scope, which empties the caches for
+// every workgroup of the XCD.  Few rows: PAST (16 sequences of 2000 8-bit keys 21 us, 30 with the acquire); 128 rows of k_paged_chunk have
+// enough to read for the acquire (256 rows after 2000 keys 46 us, 53 with PAST).
+template <bool PAST> __device__ __forceinline__ float2 join_load2(const float2 *p) {
+    if constexpr (PAST) return ld_coherent2(p);
+    else return *p;
+}
+template <bool PAST> __device__ __forceinline__ f32x4e_t join_load4(const float *p) {
+    if constexpr (PAST) return ld_coherent4(p);
+    else return *(gptr<f32x4e_t>)p;
+}
+
 // Whether this workgroup is the last of a unit's `used` to have written its part (its stores were st_coherent); leaves the ticket at zero
+template <bool PAST>
 __device__ __forceinline__ bool paged_last(const PagedAttn &c, size_t unit, int used, int *shared) {
     wait_stores();
     __syncthreads();
-    if (threadIdx.x == 0) *shared = __hip_atomic_fetch_add(c.tickets + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1;
+    int *ticket = c.tickets + unit * kPagedTicketInts;
+    if (threadIdx.x == 0) *shared = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == used - 1;
     __syncthreads();
     if (!*shared) return false;
-    if (threadIdx.x == 0) st_coherent(c.tickets + unit, 0);
-    // what the others wrote through is read from here on (each thread drops what it may hold of it)
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    if (threadIdx.x == 0) st_coherent(ticket, 0);
+    if constexpr (!PAST) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     return true;
 }
 
@@ -642,7 +665,7 @@ __device__ __forceinline__ bool paged_last(const PagedAttn &c, size_t unit, int 
 // sums.  A thread has FLIGHT vectors on their way at a time, P parts of FLIGHT / P of its own (the last part again where there are fewer than P): this
 // is one workgroup's work while others may be done, and latency is what it costs.
 struct PagedWhere { int row, d; };
-template <typename OT, int HD, int P, int FLIGHT, typename F, typename G>
+template <typename OT, int HD, int P, int FLIGHT, bool PAST, typename F, typename G>
 __device__ __forceinline__ void paged_join_by(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int used, int items, size_t part_vecs, const float2 *table, F place_of, G where) {
     constexpr int kItems = FLIGHT / P;
     for (int e0 = (int)threadIdx.x; e0 < items; e0 += 256 * kItems) {
@@ -664,7 +687,7 @@ __device__ __forceinline__ void paged_join_by(const PagedAttn &c, const PagedSeq
                 for (int i = 0; i < P; ++i) {
                     x[k][i] = f32x4e_t{0.f, 0.f, 0.f, 0.f};
                     if (where(min(e0 + 256 * k, items - 1)).row < t.rows)        // the others were not written
-                        x[k][i] = ((gptr<f32x4e_t>)c.part_o)[(size_t)place_of(min(i0 + i, used - 1)) * part_vecs + min(e0 + 256 * k, items - 1)];
+                        x[k][i] = join_load4<PAST>(c.part_o + ((size_t)place_of(min(i0 + i, used - 1)) * part_vecs + min(e0 + 256 * k, items - 1)) * 4);
                 }
 #pragma unroll
             for (int k = 0; k < kItems; ++k) {
@@ -687,14 +710,14 @@ __device__ __forceinline__ void paged_join_by(const PagedAttn &c, const PagedSeq
         }
     }
 }
-template <typename OT, int HD, int FLIGHT, typename F, typename G>
+template <typename OT, int HD, int FLIGHT, bool PAST, typename F, typename G>
 __device__ __forceinline__ void paged_join(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int used, int tile_rows, int items, float2 *table, F place_of, G where) {
     const size_t part_vecs = (size_t)tile_rows * (HD / 4);
-    for (int e = (int)threadIdx.x; e < used * t.rows; e += 256) table[e] = c.part_ml[(size_t)place_of(e / t.rows) * tile_rows + e % t.rows];
+    for (int e = (int)threadIdx.x; e < used * t.rows; e += 256) table[e] = join_load2<PAST>(c.part_ml + (size_t)place_of(e / t.rows) * tile_rows + e % t.rows);
     __syncthreads();
-    if (used <= 4) paged_join_by<OT, HD, 4, FLIGHT>(c, s, t, h, used, items, part_vecs, table, place_of, where);
-    else if (used <= 8) paged_join_by<OT, HD, 8, FLIGHT>(c, s, t, h, used, items, part_vecs, table, place_of, where);
-    else paged_join_by<OT, HD, FLIGHT, FLIGHT>(c, s, t, h, used, items, part_vecs, table, place_of, where);
+    if (used <= 4) paged_join_by<OT, HD, 4, FLIGHT, PAST>(c, s, t, h, used, items, part_vecs, table, place_of, where);
+    else if (used <= 8) paged_join_by<OT, HD, 8, FLIGHT, PAST>(c, s, t, h, used, items, part_vecs, table, place_of, where);
+    else paged_join_by<OT, HD, FLIGHT, FLIGHT, PAST>(c, s, t, h, used, items, part_vecs, table, place_of, where);
 }
 
 // Sum over the lanes up to this one, by moves between lanes (DPP: within rows of 16, then row to row)
@@ -905,9 +928,9 @@ __global__ __launch_bounds__(256, (NB * HD < 256 && sizeof(CT) < 4) || HD == 32 
         }
         if (part) {
             const int w0 = u.first / share, used = (u.first + u.groups - 1) / share - w0 + 1;
-            if (paged_last(c, ((size_t)(pair / c.row_tiles) * c.a.n_kv + h) * c.row_tiles + pair % c.row_tiles, used, &last_one)) {
+            if (paged_last<true>(c, ((size_t)(pair / c.row_tiles) * c.a.n_kv + h) * c.row_tiles + pair % c.row_tiles, used, &last_one)) {
                 const int skew = u.first == w0 * share ? 0 : 1;
-                paged_join<OT, HD, 32>(c, s, t, h, used, kRows, t.rows * (HD / 4), (float2 *)lds, [&](int i) { return 2 * (w0 + i) + (i == 0 ? skew : 0); },
+                paged_join<OT, HD, 32, true>(c, s, t, h, used, kRows, t.rows * (HD / 4), (float2 *)lds, [&](int i) { return 2 * (w0 + i) + (i == 0 ? skew : 0); },
                                          [](int e) { return PagedWhere{e / (HD / 4), e % (HD / 4) * 4}; });
             }
         }

@@ -11,7 +11,8 @@ constexpr int kChunkKeys = 64;       // keys of a tile
 constexpr int kChunkRows = 128;      // rows of a workgroup, 32 to a wave
 
 // Four waves take 32 rows each of a tile of 128, all of them every tile of 64 keys, which lands in LDS while the one before is
-// worked on (a bf16 cache: straight from memory, 1 KB a request; an 8-bit cache: through registers, where it becomes bf16).
+// worked on (a bf16 cache: straight from memory, 1 KB a request; an 8-bit cache: its codes, which each
+// wave turns into bf16 for the quarter of the keys that it asked for; in registers meanwhile, they cost 50 spilled ones).
 //   S^T = K Q^T with 32x32x16 products: lane (n, h) = (lane & 31, lane >> 5) gets row n's scores for keys 8 i + 4 h + 0..3, i = 0..3, of a block
 //   of 32: its statistics are its own up to one exchange of the wave's halves, and the scores of 16 keys, rounded to bf16, are the
 //   operand that O^T = V^T P^T wants if V's keys are taken in the same order.  V^T's operand comes from LDS by transposing reads.
@@ -25,10 +26,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
     constexpr bool F8 = sizeof(CT) == 1;
     constexpr int kRowBytes = HD * 2, kHalf = kChunkKeys * kRowBytes, kBuf = 2 * kHalf;    // K, then V
     constexpr int KS = HD / 16, CB = HD / 32;
-    constexpr int kReq = HD / 32;                                        // direct requests per wave, tile and operand
+    constexpr int kReq = F8 ? HD / 64 : HD / 32;                         // requests of 1 KB per wave, tile and operand (8-bit HD 32: one for both)
     constexpr int EB = HD / 4 < 16 ? HD / 4 : 16, NL = HD / 4 / EB;      // 8-bit: bytes of a load, loads per lane, tile and operand
-    static_assert(paged_many_splits(HD) * kChunkRows * 8 <= 2 * kBuf, "the table of the join lies there too");
-    __shared__ __align__(1024) char lds[2 * kBuf];
+    static_assert(paged_many_splits(HD) * kChunkRows * 8 <= kBuf, "the table of the join lies there too");
+    // an 8-bit cache: one tile as bf16, and per wave two tiles' codes and exponents as they came
+    constexpr int kCodes = 2 * 16 * HD, kRaw = kCodes + 256, kRawRequests = (HD == 32 ? 1 : 2 * kReq) + 1;
+    __shared__ __align__(1024) char lds[F8 ? kBuf + 8 * kRaw : 2 * kBuf];
     __shared__ int last_one;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n = lane & 31, hh = lane >> 5;
@@ -66,18 +69,16 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
         for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     float m = -INFINITY, l = 0.f;
 
-    // where this lane reads: K's piece 2 i + hh of key n; V's four elements of keys 4 hh + (lane & 15) / 4 (+ 8)
+    // where this lane reads: K's piece 2 i + hh of key n at k_at ^ 32 i; V's four elements 32 i + .. of keys 4 hh + (lane & 15) / 4 (+ 8) at v_at[..] ^ 64 i
+    // (rows of LDS start at multiples of their size, so that the permuted piece is an exclusive or away)
     const uint32_t base = lds_address(lds);
-    uint32_t k_at[KS], v_at[CB][2];
+    const uint32_t k_at = base + n * kRowBytes + ((hh ^ lds_swizzle<kRowBytes>(n)) << 4);
+    uint32_t v_at[2];
 #pragma unroll
-    for (int i = 0; i < KS; ++i) k_at[i] = base + n * kRowBytes + (((2 * i + hh) ^ lds_swizzle<kRowBytes>(n)) << 4);
-#pragma unroll
-    for (int i = 0; i < CB; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int key = 8 * e + 4 * hh + ((lane & 15) >> 2), piece = 4 * i + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-            v_at[i][e] = base + kHalf + key * kRowBytes + ((piece ^ lds_swizzle<kRowBytes>(key)) << 4) + (lane & 1) * 8;
-        }
+    for (int e = 0; e < 2; ++e) {
+        const int key = 8 * e + 4 * hh + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+        v_at[e] = base + kHalf + key * kRowBytes + ((piece ^ lds_swizzle<kRowBytes>(key)) << 4) + (lane & 1) * 8;
+    }
 
     // ---- staging.  Wave w brings keys 16 w .. 16 w + 15 of every tile.  The pages of 16 tiles are looked up at a time (lane 4 i + g: tile i, keys 16 g).
     const int page_mask = (1 << c.a.page_shift) - 1;
@@ -90,67 +91,65 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
     };
     int pages = look_up(0), pages_next = count > 16 ? look_up(16) : -1;
     uint64_t held = __ballot(pages >= 0);
-    int staged_valid = 0;                        // bit g: keys 16 g of the tile staged last have a page
-    Raw<EB> raw[2][F8 ? NL : 1];
-    uint32_t raw_scale[2][F8 ? NL : 1];
-    uint32_t from[kReq];
-    if constexpr (!F8) {
+    uint32_t from[F8 ? 1 : kReq];
 #pragma unroll
-        for (int i = 0; i < kReq; ++i) {
-            const int at = i * 1024 + lane * 16, r = at / kRowBytes, piece = at % kRowBytes >> 4;
-            from[i] = r * kRowBytes + ((piece ^ lds_swizzle<kRowBytes>(r)) << 4);
-        }
+    for (int i = 0; i < (F8 ? 1 : kReq); ++i) {
+        const int at = i * 1024 + lane * 16, r = at / kRowBytes, piece = at % kRowBytes >> 4;
+        from[i] = F8 ? lane * 16 : r * kRowBytes + ((piece ^ lds_swizzle<kRowBytes>(r)) << 4);
     }
-    auto request = [&](int i) {
+    const uint32_t raw = base + kBuf + wave * 2 * kRaw;                  // 8-bit: this wave's codes
+    auto request = [&](int i) {                  // bit g of the answer: keys 16 g of the tile have a page
         if ((i & 15) == 0 && i) {
             pages = pages_next;
             held = __ballot(pages >= 0);
             pages_next = i + 16 < count ? look_up(i + 16) : -1;
         }
-        staged_valid = (int)(held >> (4 * (i & 15))) & 15;
         const int page = max(__builtin_amdgcn_readlane(pages, 4 * (i & 15) + wave), 0), pos = key_base(i) + 16 * wave;
-        const size_t vec = paged_vec(c.a, page, h, pos & page_mask);
+        const size_t vec = scalar(paged_vec(c.a, page, h, pos & page_mask));
         if constexpr (F8) {
-            const uint8_t *src[2] = {(const uint8_t *)c.a.k + vec * HD, (const uint8_t *)c.a.v + vec * HD};
-            const uint8_t *scale[2] = {c.a.ks + vec, c.a.vs + vec};
+            const uint32_t to = __builtin_amdgcn_readfirstlane(raw + (i & 1) * kRaw);
+            const char *k = (const char *)c.a.k + vec * HD, *v = (const char *)c.a.v + vec * HD;
+            if constexpr (HD == 32) request_pieces((lane < 32 ? k : v) + (lane & 31) * 16, to);
+            else
 #pragma unroll
-            for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-                for (int e = 0; e < NL; ++e) {
-                    const int at = (e * 64 + lane) * EB;
-                    raw[kv][e].load(src[kv] + at);
-                    raw_scale[kv][e] = *(gptr<uint8_t>)(scale[kv] + at / HD);
+                for (int e = 0; e < kReq; ++e) {
+                    request_tile((const bf16_t *)(k + e * 1024), from[0], to + e * 1024);
+                    request_tile((const bf16_t *)(v + e * 1024), from[0], to + 16 * HD + e * 1024);
                 }
+            request_words((lane & 4 ? c.a.vs : c.a.ks) + vec + 4 * (lane & 3), to + kCodes);
         } else {
-            const uint32_t to = base + (i & 1) * kBuf + wave * 16 * kRowBytes;
+            const uint32_t to = __builtin_amdgcn_readfirstlane(base + (i & 1) * kBuf + wave * 16 * kRowBytes);
 #pragma unroll
             for (int e = 0; e < kReq; ++e) request_tile((const bf16_t *)c.a.k + vec * HD, from[e], to + e * 1024);
 #pragma unroll
             for (int e = 0; e < kReq; ++e) request_tile((const bf16_t *)c.a.v + vec * HD, from[e], to + kHalf + e * 1024);
         }
+        return (int)(held >> (4 * (i & 15))) & 15;
     };
-    auto place = [&](int i) {                    // 8-bit: the requested tile to LDS, as bf16
+    auto place = [&](int i) {                    // 8-bit: this wave's keys of a tile that is here to the tile of bf16
         if constexpr (F8) {
+            const uint32_t codes = raw + (i & 1) * kRaw;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
                 for (int e = 0; e < NL; ++e) {
                     const int at = (e * 64 + lane) * EB, r = at / HD, piece = at % HD >> 3;
-                    const float f = exp2_of((int)raw_scale[kv][e]);
-                    const uint32_t row = base + (i & 1) * kBuf + kv * kHalf + (wave * 16 + r) * kRowBytes;
+                    uint32_t w[4];
+                    if constexpr (EB == 8) { const u32x2_t x = lds_read<u32x2_t>(codes + kv * 16 * HD + at); w[0] = x.x; w[1] = x.y; }
+                    else { const u32x4_t x = lds_read<u32x4_t>(codes + kv * 16 * HD + at); w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; }
+                    const float f = exp2_of((int)lds_read<uint8_t>(codes + kCodes + 16 * kv + r));
+                    const uint32_t row = base + kv * kHalf + (wave * 16 + r) * kRowBytes;
 #pragma unroll
-                    for (int x = 0; x < EB / 8; ++x) {
-                        const uint32_t a = raw[kv][e].w[2 * x], b = raw[kv][e].w[2 * x + 1];
+                    for (int x = 0; x < EB / 8; ++x)
                         *(__attribute__((address_space(3))) u32x4_t *)(uintptr_t)(row + (((piece + x) ^ lds_swizzle<kRowBytes>(r)) << 4)) =
-                            u32x4_t{fp8_bf16x2<false>(a, f), fp8_bf16x2<true>(a, f), fp8_bf16x2<false>(b, f), fp8_bf16x2<true>(b, f)};
-                    }
+                            u32x4_t{fp8_bf16x2<false>(w[2 * x], f), fp8_bf16x2<true>(w[2 * x], f), fp8_bf16x2<false>(w[2 * x + 1], f), fp8_bf16x2<true>(w[2 * x + 1], f)};
                 }
         }
     };
 
     auto work = [&](int i, int valid, auto edge_c) {
         constexpr bool EDGE = decltype(edge_c)::value;
-        const uint32_t buf = (i & 1) * kBuf;
+        const uint32_t buf = F8 ? 0 : (i & 1) * kBuf;
         const int key0 = key_base(i);
         f32x16_t sc[2];
 #pragma unroll
@@ -159,7 +158,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
             for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
 #pragma unroll
             for (int e = 0; e < KS; ++e) {
-                const bf16x8_t k = *(__attribute__((address_space(3))) bf16x8_t *)(uintptr_t)(k_at[e] + buf + b * 32 * kRowBytes);
+                const bf16x8_t k = *(__attribute__((address_space(3))) bf16x8_t *)(uintptr_t)(((k_at + buf) ^ (32 * e)) + b * 32 * kRowBytes);
                 sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[e], sc[b], 0, 0, 0);
             }
         }
@@ -210,11 +209,11 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
                 if constexpr (kLow) pl = u32x4_t{p_lo[b][4 * k], p_lo[b][4 * k + 1], p_lo[b][4 * k + 2], p_lo[b][4 * k + 3]};
 #pragma unroll
                 for (int x = 0; x < CB; ++x) {
-                    const uint32_t at = buf + (2 * b + k) * 16 * kRowBytes;
+                    const uint32_t at = (2 * b + k) * 16 * kRowBytes;
                     using tr_t = __attribute__((address_space(3))) bf16x4_t;
                     union { bf16x4_t v[2]; u32x4_t w; } a;
-                    a.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(v_at[x][0] + at));
-                    a.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(v_at[x][1] + at));
+                    a.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(((v_at[0] + buf) ^ (64 * x)) + at));
+                    a.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(((v_at[1] + buf) ^ (64 * x)) + at));
                     if constexpr (EDGE) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -250,21 +249,24 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
         }
     };
 
-    if (count > 0) request(0);
-    if constexpr (F8) {
-        place(0);
-        if (count > 1) { /* the next tile's words wait in registers */ }
-    }
-    int valid = staged_valid;
-    if constexpr (F8) { if (count > 1) request(1); }
+    int valid = 0, valid_next = 0;
+    if (count > 0) valid = request(0);
+    if constexpr (F8) { if (count > 1) valid_next = request(1); }
     for (int i = 0; i < count; ++i) {
-        // tile i has landed for every wave, and every wave is done with the buffer of tile i - 1
-        if constexpr (F8) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        int valid_next = staged_valid;
-        if constexpr (!F8) {
-            if (i + 1 < count) request(i + 1);
-            valid_next = staged_valid;
+        int valid_then = 0;
+        if constexpr (F8) {
+            // this wave's codes are here, and every wave is done with the tile before; then every wave has placed its keys
+            if (i + 1 < count) wait_requests<kRawRequests>();
+            else wait_requests<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            place(i);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (i + 2 < count) valid_then = request(i + 2);
+            asm volatile("s_barrier" ::: "memory");
+        } else {
+            // tile i has landed for every wave, and every wave is done with the buffer of tile i - 1
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (i + 1 < count) valid_next = request(i + 1);
         }
         const int key0 = key_base(i), last = key0 + kChunkKeys - 1;
         const bool skip = w_rows == 0 || key0 > p_hi || (c.window && key0 >= c.sinks && p_lo - last >= c.window);
@@ -273,13 +275,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
             if (whole) work(i, valid, std::false_type{});
             else work(i, valid, std::true_type{});
         }
-        if constexpr (F8) {
-            if (i + 1 < count) place(i + 1);
-            valid_next = staged_valid;
-            if (i + 2 < count) request(i + 2);
-        }
         valid = valid_next;
+        valid_next = valid_then;
     }
+    __syncthreads();
 
     // ---- the row's sum, and what goes out
     const auto sums = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
@@ -319,8 +318,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
             st_coherent(pm + 1, l);
         }
     }
-    if (!paged_last(c, unit, used, &last_one)) return;
-    paged_join<bf16_t, HD, 16>(c, s, t, h, used, kChunkRows, kChunkRows * (HD / 4), (float2 *)lds, [&](int i) { return unit * c.splits + i; },
+    if (!paged_last<false>(c, unit, used, &last_one)) return;
+    paged_join<bf16_t, HD, 16, false>(c, s, t, h, used, kChunkRows, kChunkRows * (HD / 4), (float2 *)lds, [&](int i) { return unit * c.splits + i; },
                                [](int e) { return PagedWhere{e / (CB * 256) * 32 + (e & 31), e / 256 % CB * 32 + e / 64 % 4 * 8 + (e & 32) / 8}; });
 }
 

@@ -14,8 +14,8 @@ constexpr int paged_few_rows(int head_dim) { return head_dim == 128 ? 32 : 64; }
 // Keys a row sees at most up to which k_paged_chunk takes two bf16 terms of every probability (its comment has both sides)
 constexpr int kPagedTwoTerms = 4096;
 
-// Ranges of keys of k_paged_chunk: their maxima and sums are joined in the LDS of two key tiles
-constexpr int paged_many_splits(int head_dim) { return head_dim / 2; }
+// Ranges of keys of k_paged_chunk at most: their maxima and sums are joined in the LDS of a key tile
+constexpr int paged_many_splits(int head_dim) { return head_dim / 4; }
 
 // A launch: rows a workgroup takes, tiles of rows per KV head, ranges of keys per tile
 struct PagedPlan {
@@ -53,9 +53,9 @@ constexpr long kPagedMaxPairs = 1024;      // pairs a wave adds up before it sta
 // Groups (128 keys) a workgroup starts for at least
 constexpr int kPagedMinShare = 2;
 // Units of up to this many groups go to a workgroup each: cutting them saves less time than adding up the shares and joining the parts takes
-// (16 sequences of 1000 8-bit keys: 18 us whole, 27 in shares; of 8000: 103 and 56).  Fewer units than kPagedManyUnits leave most of the device idle:
-// there up to half as many (one sequence of 1000 keys, 8 KV heads: 17 whole, 13 in shares).
-constexpr long kPagedWholeGroups = 8, kPagedManyUnits = 32;
+// (4 sequences of 400 8-bit keys: 10.8 us whole, 11.6 in shares; of 700: 14.7 and 12.2).  Where every KV head has several tiles of rows a join has more to read, and a
+// unit is cut only if it is longer than kPagedWholeTiles and the units do not fill the device (float prompts of 3 x 500: 18.3 whole, 21.5 in shares; 4 x 2000: 141 and 211).
+constexpr long kPagedWholeGroups = 3, kPagedWholeTiles = 8;
 
 // `capacity`: positions a row of the page table reaches, whatever max_kv says; `resident`: workgroups of the kernel the device holds at once
 inline PagedShares paged_few(int batch, int n_kv, long rows, int nb, int group, int max_kv, long capacity, int window, int sinks, long resident) {
@@ -65,7 +65,7 @@ inline PagedShares paged_few(int batch, int n_kv, long rows, int nb, int group, 
     const long pairs = (long)batch * p.row_tiles;
     p.units = pairs * n_kv;
     const long each = (paged_keys(16 * nb, 32, group, max_kv, window, sinks) + 127) / 128;
-    const bool whole = each <= (p.units >= kPagedManyUnits ? kPagedWholeGroups : kPagedWholeGroups / 2) || (p.row_tiles > 1 && p.units >= resident);
+    const bool whole = each <= kPagedWholeGroups || (p.row_tiles > 1 && (each <= kPagedWholeTiles || p.units >= resident));
     p.pairs = !whole && pairs <= kPagedMaxPairs && p.units * ((capacity + 127) / 128) < 1l << 30 ? (int)pairs : 0;
     p.min_share = kPagedMinShare;
     p.groups = p.pairs ? std::max(1l, std::min(resident, (p.units * each + p.min_share - 1) / p.min_share)) : p.units;
@@ -91,11 +91,13 @@ inline int paged_blocks(bool f32, long rows, int nb_max, double work, double kv_
     return nb_max;
 }
 
-// Workspace of a launch: a ticket per unit (to a multiple of 64), then every part's maxima and sums, then its outputs
+// A ticket has a cache line of its own (256 arrivals at 8 tickets side by side made a call of 16 us 2 us longer)
+constexpr int kPagedTicketInts = 32;
+// Workspace of a launch: a ticket per unit, then every part's maxima and sums, then its outputs
 inline unsigned long long paged_workspace(long units, long parts, int tile_rows, int head_dim) {
     if (parts == 0) return 0;
     const unsigned long long rows = (unsigned long long)parts * tile_rows;
-    return ((unsigned long long)units + 63) / 64 * 256 + rows * 8 + rows * head_dim * 4;
+    return (unsigned long long)units * kPagedTicketInts * 4 + rows * 8 + rows * head_dim * 4;
 }
 
 // k_paged_chunk: two workgroups fit a compute unit
