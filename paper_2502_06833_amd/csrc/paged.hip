@@ -107,19 +107,20 @@ ead_status copy_rows(const ead_paged_cache *cache, const ead_paged_batch *batch,
     PAGED_TRY(rows_of(k, dtype, "k", &c.k));
     PAGED_TRY(rows_of(v, dtype, "v", &c.v));
     c.a = args_of(cache, batch);
-    while (c.tb < 4 && (2 << c.tb) <= batch->max_q) ++c.tb;
-    const long vecs = (((long)batch->max_q + (1 << c.tb) - 1) >> c.tb << c.tb) * cache->n_kv_heads, per = 256 / (cache->head_dim / 8);
+    const long vecs = (long)batch->max_q * cache->n_kv_heads, per = 256 / (cache->head_dim / 8);
+    const bool stream = paged_copy_streams(batch->rows, cache->n_kv_heads, cache->head_dim, element_bytes(dtype) + element_bytes(cache->dtype));
     const dim3 grid((unsigned)std::max(1l, (vecs + per - 1) / per), (unsigned)batch->batch);
     with_cache(cache, [&](auto ct, auto hd) {
         using CT = decltype(ct);
         constexpr int HD = decltype(hd)::value;
-        if (write) {
-            if (dtype == EAD_F32) hipLaunchKernelGGL((k_paged_write<CT, float, HD>), grid, dim3(256), 0, st, c);
-            else hipLaunchKernelGGL((k_paged_write<CT, bf16_t, HD>), grid, dim3(256), 0, st, c);
-        } else {
-            if (dtype == EAD_F32) hipLaunchKernelGGL((k_paged_read<CT, float, HD>), grid, dim3(256), 0, st, c);
-            else hipLaunchKernelGGL((k_paged_read<CT, bf16_t, HD>), grid, dim3(256), 0, st, c);
-        }
+        auto go = [&](auto rt, auto stream) {
+            using RT = decltype(rt);
+            constexpr bool STREAM = decltype(stream)::value;
+            if (write) hipLaunchKernelGGL((k_paged_write<CT, RT, HD, STREAM>), grid, dim3(256), 0, st, c);
+            else hipLaunchKernelGGL((k_paged_read<CT, RT, HD, STREAM>), grid, dim3(256), 0, st, c);
+        };
+        if (dtype == EAD_F32) { if (stream) go(0.f, std::true_type{}); else go(0.f, std::false_type{}); }
+        else { if (stream) go(bf16_t{}, std::true_type{}); else go(bf16_t{}, std::false_type{}); }
     });
     return launched(write ? "ead_paged_write" : "ead_paged_read");
 }

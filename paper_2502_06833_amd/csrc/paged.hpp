@@ -12,6 +12,7 @@
 namespace ead {
 
 struct fp8_t { uint8_t u; };      // an e4m3 code
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 struct PagedArgs {
     const void *k, *v;
@@ -83,11 +84,12 @@ struct RowsArg {
     int vec;                        // every vector starts on a 16-byte boundary
 };
 
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void load8(const T *p, int vec, float (&f)[8]) {
     if (vec) {
         Vec8<T> x;
-        x.load(p);
+        if constexpr (STREAM) x.load_stream(p);
+        else x.load(p);
         x.unpack(f);
     } else {
 #pragma unroll
@@ -99,8 +101,17 @@ __device__ __forceinline__ u32x4_t bf16x8_of(const float (&f)[8]) {
     return u32x4_t{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
 }
 
+template <bool STREAM, typename V> __device__ __forceinline__ void put(V *p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+template <bool STREAM> __device__ __forceinline__ void put8f(float *p, const float (&f)[8]) {
+    put<STREAM>((f32x4e_t *)p, f32x4e_t{f[0], f[1], f[2], f[3]});
+    put<STREAM>((f32x4e_t *)p + 1, f32x4e_t{f[4], f[5], f[6], f[7]});
+}
+
 // One vector's eight elements of this lane to the cache.  The HD / 8 lanes that share a vector call it together.
-template <typename CT, int HD>
+template <typename CT, int HD, bool STREAM>
 __device__ __forceinline__ void put8(void *pool, uint8_t *scales, size_t vec, int lane, float (&f)[8], bool live) {
     if constexpr (sizeof(CT) == 1) {
         float m = 0.f;
@@ -116,76 +127,68 @@ __device__ __forceinline__ void put8(void *pool, uint8_t *scales, size_t vec, in
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = __builtin_fabsf(f[e]) <= 3.402823466e38f ? f[e] * inv : __builtin_nanf("");
         if (live) {
-            uint2 w;
-            w.x = fp8_pack4(f[0], f[1], f[2], f[3]);
-            w.y = fp8_pack4(f[4], f[5], f[6], f[7]);
-            *(uint2 *)((uint8_t *)pool + vec * HD + lane * 8) = w;
+            put<STREAM>((u32x2_t *)((uint8_t *)pool + vec * HD + lane * 8), u32x2_t{fp8_pack4(f[0], f[1], f[2], f[3]), fp8_pack4(f[4], f[5], f[6], f[7])});
             if (lane == 0) scales[vec] = (uint8_t)ex;
         }
     } else if constexpr (sizeof(CT) == 2) {
-        if (live) *(u32x4_t *)((bf16_t *)pool + vec * HD + lane * 8) = bf16x8_of(f);
+        if (live) put<STREAM>((u32x4_t *)((bf16_t *)pool + vec * HD + lane * 8), bf16x8_of(f));
     } else {
-        if (live) store8<float>((float *)pool + vec * HD + lane * 8, f);
+        if (live) put8f<STREAM>((float *)pool + vec * HD + lane * 8, f);
     }
 }
 
-// The rows' vectors are taken in the order [block of 2^tb tokens][head][token]: with many rows a workgroup writes runs
-// of neighbouring slots, with one row per sequence (tb = 0) it takes the heads of that row.
+// The rows' vectors are taken in the order [token][head], the HD / 8 lanes of a vector side by side; blocks of 2 to 64 tokens of a head at a time, which write
+// runs of slots, took as long, and so did four vectors to a lane.  Bound by memory.  STREAM: non-temporal accesses, for calls that move more than the
+// second-level caches hold: 27000 rows of 8 heads to 8 bits 44 -> 40 us (4.4 TB/s), 55000 rows back as bf16 74 -> 67 us (5.6 TB/s; a large copy runs at 4.9).
 struct PagedCopy {
     PagedArgs a;
     RowsArg k, v;
-    int tb;
 };
-struct PagedItem { int t, h; };
-__device__ __forceinline__ PagedItem paged_item(const PagedCopy &c, int i) {
-    const int hb = i >> c.tb;
-    return {(hb / c.a.n_kv << c.tb) | (i & ((1 << c.tb) - 1)), hb % c.a.n_kv};
-}
 
-template <typename CT, typename RT, int HD>
+template <typename CT, typename RT, int HD, bool STREAM>
 __global__ __launch_bounds__(256) void k_paged_write(PagedCopy c) {
     constexpr int L = HD / 8, kVecs = 256 / L;
     const PagedSeq s = paged_seq(c.a, blockIdx.y);
-    const int total = ((s.n_rows + (1 << c.tb) - 1) >> c.tb << c.tb) * c.a.n_kv;
+    const int total = s.n_rows * c.a.n_kv;
     const int lane = (int)threadIdx.x % L;
     for (int i = (int)blockIdx.x * kVecs + (int)threadIdx.x / L; i < total; i += (int)gridDim.x * kVecs) {
-        const PagedItem it = paged_item(c, i);
-        const int pos = s.first + it.t;
-        bool live = it.t < s.n_rows && pos >= 0;
+        const int t = i / c.a.n_kv, h = i % c.a.n_kv, pos = s.first + t;
+        bool live = pos >= 0;
         float fk[8] = {}, fv[8] = {};
         size_t vec = 0;
         if (live) {
-            const size_t row = (size_t)(s.row0 + it.t);
-            load8((const RT *)c.k.p + row * c.k.row_stride + it.h * c.k.head_stride + lane * 8, c.k.vec, fk);
-            load8((const RT *)c.v.p + row * c.v.row_stride + it.h * c.v.head_stride + lane * 8, c.v.vec, fv);
+            const size_t row = (size_t)(s.row0 + t);
+            load8<STREAM>((const RT *)c.k.p + row * c.k.row_stride + h * c.k.head_stride + lane * 8, c.k.vec, fk);
+            load8<STREAM>((const RT *)c.v.p + row * c.v.row_stride + h * c.v.head_stride + lane * 8, c.v.vec, fv);
             const int page = paged_page(c.a, s, pos);
             live = page >= 0;
-            vec = paged_vec(c.a, max(page, 0), it.h, pos & ((1 << c.a.page_shift) - 1));
+            vec = paged_vec(c.a, max(page, 0), h, pos & ((1 << c.a.page_shift) - 1));
         }
-        put8<CT, HD>((void *)c.a.k, (uint8_t *)c.a.ks, vec, lane, fk, live);
-        put8<CT, HD>((void *)c.a.v, (uint8_t *)c.a.vs, vec, lane, fv, live);
+        put8<CT, HD, STREAM>((void *)c.a.k, (uint8_t *)c.a.ks, vec, lane, fk, live);
+        put8<CT, HD, STREAM>((void *)c.a.v, (uint8_t *)c.a.vs, vec, lane, fv, live);
     }
 }
 
-template <typename CT, int HD>
+template <typename CT, int HD, bool STREAM>
 __device__ __forceinline__ void get8(const void *pool, const uint8_t *scales, size_t vec, int lane, float (&f)[8]) {
     if constexpr (sizeof(CT) == 1) {
         typedef float f32x2_t __attribute__((ext_vector_type(2)));
-        const uint2 w = *(const uint2 *)((const uint8_t *)pool + vec * HD + lane * 8);
+        const u32x2_t *p = (const u32x2_t *)((const uint8_t *)pool + vec * HD + lane * 8);
+        const u32x2_t w = STREAM ? __builtin_nontemporal_load(p) : *p;
         const float scale = exp2_of(scales[vec]);
         const f32x2_t p0 = __builtin_amdgcn_cvt_pk_f32_fp8(w.x, false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(w.x, true);
         const f32x2_t p2 = __builtin_amdgcn_cvt_pk_f32_fp8(w.y, false), p3 = __builtin_amdgcn_cvt_pk_f32_fp8(w.y, true);
         f[0] = p0.x * scale; f[1] = p0.y * scale; f[2] = p1.x * scale; f[3] = p1.y * scale;
         f[4] = p2.x * scale; f[5] = p2.y * scale; f[6] = p3.x * scale; f[7] = p3.y * scale;
     } else {
-        load8((const CT *)pool + vec * HD + lane * 8, 1, f);
+        load8<STREAM>((const CT *)pool + vec * HD + lane * 8, 1, f);
     }
 }
-template <typename RT>
+template <bool STREAM, typename RT>
 __device__ __forceinline__ void set8(RT *p, int vec, const float (&f)[8]) {
     if (vec) {
-        if constexpr (sizeof(RT) == 2) *(u32x4_t *)p = bf16x8_of(f);
-        else store8<float>(p, f);
+        if constexpr (sizeof(RT) == 2) put<STREAM>((u32x4_t *)p, bf16x8_of(f));
+        else put8f<STREAM>(p, f);
         return;
     }
 #pragma unroll
@@ -195,26 +198,24 @@ __device__ __forceinline__ void set8(RT *p, int vec, const float (&f)[8]) {
     }
 }
 
-template <typename CT, typename RT, int HD>
+template <typename CT, typename RT, int HD, bool STREAM>
 __global__ __launch_bounds__(256) void k_paged_read(PagedCopy c) {
     constexpr int L = HD / 8, kVecs = 256 / L;
     const PagedSeq s = paged_seq(c.a, blockIdx.y);
-    const int total = ((s.n_rows + (1 << c.tb) - 1) >> c.tb << c.tb) * c.a.n_kv;
+    const int total = s.n_rows * c.a.n_kv;
     const int lane = (int)threadIdx.x % L;
     for (int i = (int)blockIdx.x * kVecs + (int)threadIdx.x / L; i < total; i += (int)gridDim.x * kVecs) {
-        const PagedItem it = paged_item(c, i);
-        if (it.t >= s.n_rows) continue;
-        const int pos = s.first + it.t;
+        const int t = i / c.a.n_kv, h = i % c.a.n_kv, pos = s.first + t;
         const int page = pos >= 0 ? paged_page(c.a, s, pos) : -1;
         float fk[8] = {}, fv[8] = {};
         if (page >= 0) {
-            const size_t vec = paged_vec(c.a, page, it.h, pos & ((1 << c.a.page_shift) - 1));
-            get8<CT, HD>(c.a.k, c.a.ks, vec, lane, fk);
-            get8<CT, HD>(c.a.v, c.a.vs, vec, lane, fv);
+            const size_t vec = paged_vec(c.a, page, h, pos & ((1 << c.a.page_shift) - 1));
+            get8<CT, HD, STREAM>(c.a.k, c.a.ks, vec, lane, fk);
+            get8<CT, HD, STREAM>(c.a.v, c.a.vs, vec, lane, fv);
         }
-        const size_t row = (size_t)(s.row0 + it.t);
-        set8((RT *)c.k.p + row * c.k.row_stride + it.h * c.k.head_stride + lane * 8, c.k.vec, fk);
-        set8((RT *)c.v.p + row * c.v.row_stride + it.h * c.v.head_stride + lane * 8, c.v.vec, fv);
+        const size_t row = (size_t)(s.row0 + t);
+        set8<STREAM>((RT *)c.k.p + row * c.k.row_stride + h * c.k.head_stride + lane * 8, c.k.vec, fk);
+        set8<STREAM>((RT *)c.v.p + row * c.v.row_stride + h * c.v.head_stride + lane * 8, c.v.vec, fv);
     }
 }
 
@@ -283,7 +284,6 @@ template <int N> struct Raw {
 
 // ---- LDS by its address ----------------------------------------------------------------------------
 using lds_byte = __attribute__((address_space(3))) char;
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(lds_byte *)p; }
 template <typename T> __device__ __forceinline__ T lds_read(uint32_t at) { return *(__attribute__((address_space(3))) T *)(uintptr_t)at; }
 // 4 bytes per lane, each from its own address, to LDS at lds + 4 lane (M0 as in request_tile)
@@ -745,7 +745,7 @@ struct PagedUnit {
 //  Where there are more pairs than a wave adds up in a reasonable time, a workgroup takes a unit (c.pairs = 0).
 //  A workgroup has NB blocks of 16 rows and all four waves work on the same ones, each on every fourth key tile; they are joined through LDS.
 template <typename CT, int HD, int NB>
-__global__ __launch_bounds__(256, (NB * HD < 256 && sizeof(CT) < 4) || HD == 32 ? 2 : 1) void k_paged_attn(PagedAttn c) {
+__global__ __launch_bounds__(256, (NB * HD < 256 && PagedWave<CT, HD, NB>::kRing * PagedWave<CT, HD, NB>::kTile <= 20480) ? 2 : 1) void k_paged_attn(PagedAttn c) {
     using W = PagedWave<CT, HD, NB>;
     using OT = typename std::conditional<sizeof(CT) == 4, float, bf16_t>::type;
     constexpr int kRows = NB * 16, kWaveBytes = W::kRing * W::kTile, kJoin = 4 * 16 * (HD + 4) * 4;

@@ -5,6 +5,9 @@
 namespace ead {
 
 
+// Whether a write or a read moves more than stays in the second-level caches (32 MB) for who comes next
+inline bool paged_copy_streams(long rows, int n_kv, int head_dim, int bytes) { return 2.0 * rows * n_kv * head_dim * bytes > 64e6; }
+
 // Blocks of 16 rows that a wave's registers hold at most
 constexpr int paged_max_blocks(int head_dim) { return head_dim == 128 ? 2 : 4; }
 
