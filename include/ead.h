@@ -278,7 +278,7 @@ void ead_gate_destroy(ead_gate *g);
 /* The cache of one attention layer, in pages of the caller's device memory:
  *   k, v              [n_pages][n_kv_heads][page_size][head_dim] of `dtype`, 16-byte aligned
  *   k_scale, v_scale  [n_pages][n_kv_heads][page_size], EAD_FP8 only (null otherwise): the head's
- *                     vector at that position is its e4m3 codes times 2^(scale - 127)
+ *                     vector at that position is its e4m3 codes times 2^(scale - 127), scale 1 .. 254
  * page_size is 16, 32, 64, 128 or 256; head_dim 32, 64 or 128.  Rounding to EAD_FP8 takes the smallest
  * power of two that brings the vector's largest finite magnitude to 448 or less, so codes times
  * scale are exact in bf16; elements that are not finite become NaN. */

@@ -109,7 +109,7 @@ ead_status copy_rows(const ead_paged_cache *cache, const ead_paged_batch *batch,
     c.a = args_of(cache, batch);
     const long vecs = (long)batch->max_q * cache->n_kv_heads, per = 256 / (cache->head_dim / 8);
     const bool stream = paged_copy_streams(batch->rows, cache->n_kv_heads, cache->head_dim, element_bytes(dtype) + element_bytes(cache->dtype));
-    const dim3 grid((unsigned)std::max(1l, (vecs + per - 1) / per), (unsigned)batch->batch);
+    const dim3 grid((unsigned)std::clamp((vecs + per - 1) / per, 1l, 1l << 20), (unsigned)batch->batch);     // the kernels go on past their grid
     with_cache(cache, [&](auto ct, auto hd) {
         using CT = decltype(ct);
         constexpr int HD = decltype(hd)::value;
@@ -163,6 +163,9 @@ FewKernel few_kernel(const ead_paged_cache *c, int nb) {
     return k;
 }
 
+double g_small_work = kPagedSmallWork;                 // ead_test_paged's
+bool g_always_shares = false;
+
 // The launches of a call: sequences with few rows (of a float32 cache: all), then those with many
 struct PagedCall {
     bool few, many, two;
@@ -172,21 +175,26 @@ struct PagedCall {
     PagedPlan m;
     uint64_t f_bytes, m_bytes;
 };
-PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_paged_attn *at) {
-    const int held = (int)std::min((long)b->max_kv, (long)b->table_width * c->page_size), group = at->n_heads / c->n_kv_heads, cus = compute_units();
+PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_paged_attn *given) {
+    const long capacity = (long)b->table_width * c->page_size;
+    ead_paged_attn seen = *given;
+    if (seen.window >= capacity) seen.window = 0;            // every position is in it
+    const ead_paged_attn *at = &seen;
+    const int held = (int)std::min((long)b->max_kv, capacity), group = at->n_heads / c->n_kv_heads, cus = compute_units();
     const bool f32 = c->dtype == EAD_F32;
     const long rows = (long)b->max_q * group;
     PagedCall p{};
     const double work = paged_work(b->batch, c->n_kv_heads, c->head_dim, group, rows, held, at->window, at->sinks);
     const double kv_bytes = 2.0 * b->batch * c->n_kv_heads * c->head_dim * element_bytes(c->dtype) * (double)paged_keys(16, 32, group, held, at->window, at->sinks);
-    p.few_rows = f32 || work <= kPagedSmallWork ? 0x7FFFFFFF : paged_few_rows(c->head_dim);
+    p.few_rows = f32 || work <= g_small_work ? 0x7FFFFFFF : paged_few_rows(c->head_dim);
     p.few = (long)b->min_q * group <= p.few_rows;
     p.many = rows > p.few_rows;
     if (p.few) {
         const long few = std::min(rows, (long)p.few_rows);
         const int nb = paged_blocks(f32, few, paged_max_blocks(c->head_dim), work, kv_bytes);
         p.kernel = few_kernel(c, nb);
-        p.f = paged_few(b->batch, c->n_kv_heads, few, nb, group, held, (long)b->table_width * c->page_size, at->window, at->sinks, p.kernel.resident);
+        p.f = paged_few(b->batch, c->n_kv_heads, few, nb, group, held, capacity, at->window, at->sinks, p.kernel.resident,
+                        g_always_shares ? 0 : kPagedWholeGroups, g_always_shares ? 0 : kPagedWholeTiles);
         p.f_bytes = paged_workspace(p.f.units, p.f.parts, 16 * nb, c->head_dim);
     }
     if (p.many) {
@@ -235,6 +243,8 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     PAGED_TRY(rows_of(out, attn->dtype, "out", &c.out));
     const PagedCall p = plan_of(cache, batch, attn);
     const uint64_t need = p.f_bytes + p.m_bytes;
+    if ((p.few && p.f.groups >= 1 << 24) || (p.many && (long)p.m.row_tiles * p.m.splits * cache->n_kv_heads >= 1 << 24))
+        return refuse(EAD_ERR_SHAPE, "batch: max_q of %d rows for each of %d sequences needs 2^24 workgroups or more", batch->max_q, batch->batch);
     if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
         return refuse(EAD_ERR_INVALID_ARG, "workspace: %llu bytes, 16-byte aligned, are needed", (unsigned long long)need);
     c.a = args_of(cache, batch);
@@ -242,7 +252,7 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     c.n_heads = attn->n_heads;
     c.group = attn->n_heads / cache->n_kv_heads;
     c.c2 = attn->scale * 1.4426950408889634f;
-    c.window = attn->window;
+    c.window = attn->window >= (long)batch->table_width * cache->page_size ? 0 : attn->window;
     c.sinks = attn->sinks;
     c.few_rows = p.few_rows;
     const hipStream_t st = (hipStream_t)hip_stream;
@@ -265,6 +275,13 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
         });
     }
     return launched("ead_paged_attention");
+}
+
+// For the tests alone, in no header: the work up to which one kernel takes a call alone (-1: as ever), and whether units are always cut into shares.
+ead_status ead_test_paged(double small_work, int32_t always_shares) {
+    g_small_work = small_work < 0 ? kPagedSmallWork : small_work;
+    g_always_shares = always_shares != 0;
+    return EAD_OK;
 }
 
 }  // extern "C"

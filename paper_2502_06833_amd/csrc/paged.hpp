@@ -251,7 +251,7 @@ __device__ __forceinline__ PagedTile paged_tile(const PagedAttn &c, const PagedS
     t.rows = min(max(s.n_rows * c.group - t.r0, 0), tile_rows);
     t.p_lo = s.first + t.r0 / c.group;
     t.p_hi = s.first + (t.r0 + max(t.rows, 1) - 1) / c.group;
-    t.t_lo = c.window ? max(0, t.p_lo - c.window + 1) / KEYS : 0;
+    t.t_lo = c.window ? max(0, max(t.p_lo, 0) - c.window + 1) / KEYS : 0;
     t.n_sink = c.window ? min((min(c.sinks, s.kv) + KEYS - 1) / KEYS, t.t_lo) : 0;
     t.tiles = t.rows > 0 && t.p_hi >= 0 ? t.n_sink + max(t.p_hi / KEYS + 1 - t.t_lo, 0) : 0;
     return t;

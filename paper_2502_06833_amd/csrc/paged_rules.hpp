@@ -61,14 +61,15 @@ constexpr int kPagedMinShare = 2;
 constexpr long kPagedWholeGroups = 3, kPagedWholeTiles = 8;
 
 // `capacity`: positions a row of the page table reaches, whatever max_kv says; `resident`: workgroups of the kernel the device holds at once
-inline PagedShares paged_few(int batch, int n_kv, long rows, int nb, int group, int max_kv, long capacity, int window, int sinks, long resident) {
+inline PagedShares paged_few(int batch, int n_kv, long rows, int nb, int group, int max_kv, long capacity, int window, int sinks, long resident,
+                             long whole_groups = kPagedWholeGroups, long whole_tiles = kPagedWholeTiles) {
     PagedShares p;
     p.nb = nb;
     p.row_tiles = (int)std::max(1l, (rows + 16 * nb - 1) / (16 * nb));
     const long pairs = (long)batch * p.row_tiles;
     p.units = pairs * n_kv;
     const long each = (paged_keys(16 * nb, 32, group, max_kv, window, sinks) + 127) / 128;
-    const bool whole = each <= kPagedWholeGroups || (p.row_tiles > 1 && (each <= kPagedWholeTiles || p.units >= resident));
+    const bool whole = each <= whole_groups || (p.row_tiles > 1 && (each <= whole_tiles || (whole_tiles && p.units >= resident)));
     p.pairs = !whole && pairs <= kPagedMaxPairs && p.units * ((capacity + 127) / 128) < 1l << 30 ? (int)pairs : 0;
     p.min_share = kPagedMinShare;
     p.groups = p.pairs ? std::max(1l, std::min(resident, (p.units * each + p.min_share - 1) / p.min_share)) : p.units;

@@ -6,6 +6,7 @@ times their rounding.  The bf16 path rounds its output to bf16 (relative 2^-9 at
 term at the least (2^-9 of each summand at most, of either sign), so an element is off by at most 2^-9 |out| + 2^-9
 sum_j p_j |v_j|: the bound used is 1.05 times that plus 1e-5.  Log-sum-exps are float32 throughout: 1e-5 absolute for values up to
 some tens (exponents rounded at 2^-24 of a score of a few tens)."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -38,6 +39,17 @@ def exact_round(x, dtype):
         r = torch.where(torch.isfinite(x), r, torch.nan)
         return r * two_to(e), (e[..., 0] + 127).to(torch.uint8)
     return x.to(dtype).double(), None
+
+
+@pytest.fixture(params=["as ever", "many rows", "shares"])
+def way(request):
+    """The kernels and schedules that a call's size would not choose by itself: k_paged_chunk for all sequences of more than 32 or 64
+    rows per KV head however little work they are, and equal shares of the keys however short the contexts."""
+    L = ead.lib()
+    L.ead_test_paged.argtypes = [C.c_double, C.c_int32]
+    L.ead_test_paged(0.0 if request.param == "many rows" else -1.0, 1 if request.param == "shares" else 0)
+    yield request.param
+    L.ead_test_paged(-1.0, 0)
 
 
 class Setup:
@@ -197,7 +209,7 @@ def test_not_finite_values_stay_visible(dtype):
 
 @pytest.mark.parametrize("dtype,src", [(torch.bfloat16, torch.bfloat16), (F8, torch.bfloat16), (torch.float32, torch.float32)])
 @pytest.mark.parametrize("offset", [0, 1, 8])
-def test_strided_rows(dtype, src, offset):
+def test_strided_rows(way, dtype, src, offset):
     """Q, K and V as slices of one projection's output, at offsets that do and do not keep 16-byte alignment."""
     n_heads, n_kv, hd = 6, 2, 64
     s = Setup([7, 33], [20, 33], n_kv, hd, dtype, 32, seed=5)
@@ -232,7 +244,7 @@ HEADS = [(4, 4, 32), (14, 2, 64), (8, 1, 128), (40, 8, 128), (24, 1, 32)]
     ([17, 40, 1], [17, 300, 77], 16),                       # pieces of prompts
     ([130, 257], [130, 400], 256),
 ])
-def test_attention(dtype, heads, q_lens, kv_lens, page):
+def test_attention(way, dtype, heads, q_lens, kv_lens, page):
     n_heads, n_kv, hd = heads
     s = Setup(q_lens, kv_lens, n_kv, hd, dtype, page, seed=11)
     s.write_all()
@@ -244,7 +256,7 @@ def test_attention(dtype, heads, q_lens, kv_lens, page):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (31, 4), (64, 33), (100, 0), (5000, 7), (33, 5000)])
 @pytest.mark.parametrize("q_lens,kv_lens", [([1, 1, 1], [700, 40, 2100]), ([5, 1, 9], [700, 1, 333]), ([150, 1], [600, 900])])
-def test_window_and_sinks(dtype, window, sinks, q_lens, kv_lens):
+def test_window_and_sinks(way, dtype, window, sinks, q_lens, kv_lens):
     s = Setup(q_lens, kv_lens, 2, 64, dtype, 16, seed=window)
     s.write_all()
     q = s.queries(6, 1.5)
@@ -254,7 +266,7 @@ def test_window_and_sinks(dtype, window, sinks, q_lens, kv_lens):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n", [3, 40, 200])
-def test_rows_before_the_first_position_see_nothing(dtype, n):
+def test_rows_before_the_first_position_see_nothing(way, dtype, n):
     """More rows than positions: the first rows are at positions below 0; and sequences that hold nothing at all."""
     s = Setup([n, n, 2], [2, 0, 0], 2, 64, dtype, 16)
     s.write_all()
@@ -270,7 +282,7 @@ def test_rows_before_the_first_position_see_nothing(dtype, n):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("q_len", [1, 6, 90])
-def test_holes_are_not_seen(dtype, q_len):
+def test_holes_are_not_seen(way, dtype, q_len):
     """Pages that a window has left behind may be taken away: their table entries are holes, and nothing of them is read."""
     s = Setup([q_len], [400], 2, 64, dtype, 16, seed=2)
     s.write_all()
@@ -302,7 +314,7 @@ def test_holes_are_not_seen(dtype, q_len):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("q_len,kv", [(1, 100), (8, 100), (70, 180), (150, 150)])
-def test_what_is_masked_has_no_effect(dtype, bad, q_len, kv):
+def test_what_is_masked_has_no_effect(way, dtype, bad, q_len, kv):
     """A later token's or a forgotten token's NaN or infinity does not reach the rows that do not see it; rows that see
     it are not finite where it is."""
     window, sinks, at, old = 40, 2, kv - 1, 7
@@ -325,7 +337,7 @@ def test_what_is_masked_has_no_effect(dtype, bad, q_len, kv):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_nothing_but_nan_is_nan(dtype):
+def test_nothing_but_nan_is_nan(way, dtype):
     s = Setup([1, 1], [50, 70], 1, 64, dtype)
     s.write_all()
     q = s.queries(2)
@@ -336,7 +348,7 @@ def test_nothing_but_nan_is_nan(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_large_scores(dtype):
+def test_large_scores(way, dtype):
     """Scores of hundreds: the running maximum keeps exponentials finite, in any order of the keys."""
     s = Setup([1, 20], [900, 900], 1, 64, dtype, seed=9)
     s.write_all()
@@ -349,7 +361,7 @@ def test_large_scores(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_shared_pages_and_pieces(dtype):
+def test_shared_pages_and_pieces(way, dtype):
     """Two sequences that share their first pages; a prompt taken in one call and in pieces gives the same rows."""
     s = Setup([96], [96], 2, 64, dtype, 16, seed=6)
     s.write_all()
@@ -363,7 +375,7 @@ def test_shared_pages_and_pieces(dtype):
     assert float((got[10].double() - whole[79].double()).abs().max()) <= tol
 
 
-def test_a_long_sequence_in_a_large_pool():
+def test_a_long_sequence_in_a_large_pool(way):
     """Element offsets beyond 2^31: the last pages of a pool of 2.2e9 elements."""
     n_kv, hd, page = 8, 128, 256
     n_pages = (2 ** 31 + 2 ** 27) // (n_kv * hd * page)
@@ -387,7 +399,7 @@ def test_a_long_sequence_in_a_large_pool():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_a_graph_follows_its_lengths(dtype):
+def test_a_graph_follows_its_lengths(way, dtype):
     """A captured step (write and attention) replayed while the lengths on the device grow, against eager calls."""
     n_kv, hd, steps = 2, 64, 5
     s = Setup([1, 1], [300, 1500], n_kv, hd, dtype, 16, seed=8, stale=0.0)
@@ -423,7 +435,7 @@ def test_a_graph_follows_its_lengths(dtype):
         assert lens.tolist() == [n + 1 for n in now]
 
 
-def test_two_streams_have_their_own_workspaces():
+def test_two_streams_have_their_own_workspaces(way):
     s = Setup([1], [6000], 1, 128, torch.bfloat16, 16)
     s.write_all()
     q = s.queries(8)
@@ -439,7 +451,7 @@ def test_two_streams_have_their_own_workspaces():
     assert all(torch.equal(o, want) for o in outs)
 
 
-def test_repeated_calls_are_bit_equal():
+def test_repeated_calls_are_bit_equal(way):
     s = Setup([1, 1, 30], [3000, 77, 900], 2, 128, F8, 32)
     s.write_all()
     q = s.queries(10)
@@ -449,7 +461,7 @@ def test_repeated_calls_are_bit_equal():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-def test_bounds_that_are_too_small_stay_in_range():
+def test_bounds_that_are_too_small_stay_in_range(way):
     """max_kv and max_q below what the device arrays say: reads and writes stay inside, rows up to max_q are right."""
     s = Setup([1, 1], [900, 500], 2, 64, torch.bfloat16, 16)
     s.write_all()
@@ -461,6 +473,69 @@ def test_bounds_that_are_too_small_stay_in_range():
     s.cache.attention(q, wild)
     s.cache.read(wild)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch", [64, 65, 150, 1100])
+def test_many_sequences(way, dtype, batch):
+    """More sequences than a wave has lanes, and more than are cut into shares; some without rows, some with many."""
+    rng = np.random.default_rng(batch)
+    q_lens = rng.choice([0, 1, 1, 1, 2, 9], batch).tolist()
+    kv_lens = [int(n) + q for n, q in zip(rng.integers(0, 1500 if batch < 1000 else 60, batch), q_lens)]
+    s = Setup(q_lens, kv_lens, 2, 32, dtype, 16, seed=batch)
+    s.write_all()
+    q = s.queries(14, 1.5)
+    got, lse = s.cache.attention(q, s.batch, want_lse=True)
+    check_attention(s, q, got, lse, exact_attention(s, q))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads", [(8, 1, 32), (10, 2, 128)])
+@pytest.mark.parametrize("window,sinks", [(17, 3), (129, 0), (70, 40)])
+def test_windows_of_other_heads(way, dtype, heads, window, sinks):
+    n_heads, n_kv, hd = heads
+    s = Setup([1, 200, 33], [300, 333, 40], n_kv, hd, dtype, 64, seed=window)
+    s.write_all()
+    q = s.queries(n_heads, 1.5)
+    got, lse = s.cache.attention(q, s.batch, window=window, sinks=sinks, want_lse=True)
+    check_attention(s, q, got, lse, exact_attention(s, q, window, sinks))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("k_scale,v_scale", [(2.0 ** 40, 2.0 ** -40), (2.0 ** -60, 2.0 ** 60)])
+def test_magnitudes_far_from_one(way, dtype, k_scale, v_scale):
+    """Powers of two in K, undone in the queries, and in V: the same attention, times V's."""
+    s = Setup([1, 50], [200, 170], 2, 64, dtype, seed=3)
+    n = sum(s.kv_lens)
+    k, v = (torch.randn(n, 2, 64, generator=s.g, device=DEV) for _ in range(2))
+    s.write_all(k=k, v=v)
+    q = s.queries(6)
+    want = s.cache.attention(q, s.batch)
+    s.write_all(k=k * k_scale, v=v * v_scale)
+    got = s.cache.attention((q.float() / k_scale).to(q.dtype), s.batch)
+    assert torch.equal(got.double() / v_scale, want.double())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, F8])
+@pytest.mark.parametrize("heads", [(8, 2, 64), (4, 4, 32), (4, 1, 128)])
+def test_many_rows_over_long_contexts(dtype, heads):
+    """More than 4096 keys: one bf16 term of each probability away from the edges.  A term is off by at most 2^-8 of itself (8 significant
+    bits), and so is the output's rounding: 1.05 * 2^-8 (|out| + sum_j p_j |v_j|) + 1e-5."""
+    n_heads, n_kv, hd = heads
+    s = Setup([700, 450], [5000, 4700], n_kv, hd, dtype, 64, seed=1)
+    s.write_all()
+    q = s.queries(n_heads, 1.5)
+    L = ead.lib()
+    L.ead_test_paged.argtypes = [C.c_double, C.c_int32]
+    L.ead_test_paged(0.0, 0)
+    try:
+        got, lse = s.cache.attention(q, s.batch, want_lse=True)
+    finally:
+        L.ead_test_paged(-1.0, 0)
+    out, z, mass = exact_attention(s, q)
+    bound = 1.05 * 2.0 ** -8 * (out.abs() + mass) + 1e-5
+    assert bool(((got.double() - out).abs() <= bound).all())
+    assert float((lse.double() - z).abs().max()) <= 1e-5
 
 
 def test_refusals():
