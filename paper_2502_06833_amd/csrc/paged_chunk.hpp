@@ -20,7 +20,7 @@ constexpr int kChunkRows = 128;      // rows of a workgroup, 32 to a wave
 //  Probabilities enter the second product as bf16.  One term of each is off by up to 2^-8 of it, which beside the rounding of the output
 //  makes the result's error against 64 bits 0.0023 of its norm instead of 0.0017; a second term (what the first leaves, rounded) takes that away for
 //  half as many products again.  Rows at a mask's edge, among them all that see few keys, always have both; the other tiles have both where no row of
-//  the launch sees more than kPagedTwoTerms keys (TWO): 4096 rows over 12289 .. 16384 keys of 32 heads take 1050 us with one term, 1400 with two.
+//  the launch sees more than kPagedTwoTerms keys (TWO): 4096 rows over 12289 .. 16384 keys of 32 heads take 1020 us with one term, 1400 with two.
 template <typename CT, int HD, bool TWO>
 __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
     constexpr bool F8 = sizeof(CT) == 1;
@@ -163,12 +163,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
             }
         }
         if constexpr (EDGE) {
+            int pos = my_pos, from_key = 4 * hh;
+            asm volatile("" : "+v"(pos), "+v"(from_key));        // computed here, not kept in registers beside every tile's work (191 -> 168 us)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = key0 + 32 * b + 8 * (e >> 2) + 4 * hh + (e & 3);
-                    sc[b][e] = (valid >> (2 * b + (e >> 3)) & 1) && paged_sees(c, my_pos, key) ? sc[b][e] : -INFINITY;
+                    const int key = key0 + from_key + 32 * b + 8 * (e >> 2) + (e & 3);
+                    sc[b][e] = (valid >> (2 * b + (e >> 3)) & 1) && paged_sees(c, pos, key) ? sc[b][e] : -INFINITY;
                 }
         }
         float top = -INFINITY;
@@ -188,32 +190,33 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
                 for (int e = 0; e < 16; ++e) o[x][e] *= f;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        constexpr bool kLow = TWO || EDGE;
-        uint32_t p[2][8], p_lo[2][8];            // the probabilities' bf16 terms
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e], c.c2, -ref)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e + 1], c.c2, -ref));
-                l += x + y;
-                p[b][e] = pack_bf16(x, y);
-                if constexpr (kLow) p_lo[b][e] = pack_bf16(x - __uint_as_float(p[b][e] << 16), y - __uint_as_float(p[b][e] & 0xFFFF0000u));
-            }
+        using tr_t = __attribute__((address_space(3))) bf16x4_t;
+        union Operand { bf16x4_t v[2]; u32x4_t w; };
+        auto read_v = [&](int j, int x, Operand &a) {        // V^T's operand: dimensions 32 x .., the tile's keys 16 j ..
+            a.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(((v_at[0] + buf) ^ (64 * x)) + j * 16 * kRowBytes));
+            a.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(((v_at[1] + buf) ^ (64 * x)) + j * 16 * kRowBytes));
+        };
+        auto multiply = [&](int x, const Operand &a, const uint32_t *p) {
+            o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.w), __builtin_bit_cast(bf16x8_t, u32x4_t{p[0], p[1], p[2], p[3]}), o[x], 0, 0, 0);
+        };
         bool odd = false;
+        if constexpr (TWO || EDGE) {
+            uint32_t p[2][8], p_lo[2][8];            // the probabilities' two bf16 terms
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const u32x4_t pw = {p[b][4 * k], p[b][4 * k + 1], p[b][4 * k + 2], p[b][4 * k + 3]};
-                u32x4_t pl;
-                if constexpr (kLow) pl = u32x4_t{p_lo[b][4 * k], p_lo[b][4 * k + 1], p_lo[b][4 * k + 2], p_lo[b][4 * k + 3]};
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e], c.c2, -ref)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e + 1], c.c2, -ref));
+                    l += x + y;
+                    p[b][e] = pack_bf16(x, y);
+                    p_lo[b][e] = pack_bf16(x - __uint_as_float(p[b][e] << 16), y - __uint_as_float(p[b][e] & 0xFFFF0000u));
+                }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int x = 0; x < CB; ++x) {
-                    const uint32_t at = (2 * b + k) * 16 * kRowBytes;
-                    using tr_t = __attribute__((address_space(3))) bf16x4_t;
-                    union { bf16x4_t v[2]; u32x4_t w; } a;
-                    a.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(((v_at[0] + buf) ^ (64 * x)) + at));
-                    a.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr_t *)(uintptr_t)(((v_at[1] + buf) ^ (64 * x)) + at));
+                    Operand a;
+                    read_v(j, x, a);
                     if constexpr (EDGE) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -222,13 +225,51 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
                             a.w[e] &= (b0 ? 0xFFFF0000u : 0xFFFFFFFFu) & (b1 ? 0xFFFFu : 0xFFFFFFFFu);
                         }
                     }
-                    o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.w), __builtin_bit_cast(bf16x8_t, pw), o[x], 0, 0, 0);
-                    if constexpr (kLow) o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.w), __builtin_bit_cast(bf16x8_t, pl), o[x], 0, 0, 0);
+                    multiply(x, a, p[j >> 1] + 4 * (j & 1));
+                    multiply(x, a, p_lo[j >> 1] + 4 * (j & 1));
                 }
-            }
+        } else {
+            // With one term there are registers to read V's operands of 16 keys while those of the 16 before are multiplied, and to take the second
+            // block's exponentials beside the first one's products (4096 rows over 12289 .. 16384 keys 1045 -> 1020 us; with two terms 168 -> 179 us
+            // for 17 sequences over 8-bit pages: there the compiler's own order stands).
+            uint32_t p[2][8];
+            auto terms = [&](int b) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e], c.c2, -ref)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e + 1], c.c2, -ref));
+                    l += x + y;
+                    p[b][e] = pack_bf16(x, y);
+                }
+            };
+            Operand a[2][CB];
+            auto read_all = [&](int j) {
+#pragma unroll
+                for (int x = 0; x < CB; ++x) read_v(j, x, a[j & 1][x]);
+            };
+            auto multiply_all = [&](int j) {
+#pragma unroll
+                for (int x = 0; x < CB; ++x) multiply(x, a[j & 1][x], p[j >> 1] + 4 * (j & 1));
+            };
+            read_all(0);
+            terms(0);
+            read_all(1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply_all(0);
+            terms(1);
+            __builtin_amdgcn_sched_barrier(0);
+            read_all(2);
+            multiply_all(1);
+            __builtin_amdgcn_sched_barrier(0);
+            read_all(3);
+            multiply_all(2);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply_all(3);
+        }
         if constexpr (EDGE) {
             if (__any(odd)) {
                 // infinities and NaN, left out of the product, go to the rows that see them (PagedWave::add_odd)
+                int from_dim = 4 * hh;
+                asm volatile("" : "+v"(from_dim));
                 for (int k = 0; k < kChunkKeys; ++k) {
                     const int key = key0 + k;
                     if (!(valid >> (k >> 4) & 1) || key > p_hi) continue;
@@ -238,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
                     for (int x = 0; x < CB; ++x)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const size_t at = vec * HD + 32 * x + 8 * (e >> 2) + 4 * hh + (e & 3);
+                            const size_t at = vec * HD + 32 * x + 8 * (e >> 2) + from_dim + (e & 3);
                             float v;
                             if constexpr (F8) v = (((const uint8_t *)c.a.v)[at] & 0x7F) == 0x7F ? __builtin_nanf("") : 0.f;
                             else v = to_f32(((const CT *)c.a.v)[at]);
