@@ -765,7 +765,7 @@ __global__ __launch_bounds__(256, (NB * HD < 256 && PagedWave<CT, HD, NB>::kRing
         const PagedTile t = paged_tile<kKeyTile>(c, s, c.row_tiles == 1 ? 0 : pair % c.row_tiles, kRows);
         return t.rows == 0 ? 0 : max(1, (t.tiles + kGroup - 1) / kGroup);
     };
-    int pos = 0, end = 0, share = 1;             // (the host sees to it that all groups fit 30 bits)
+    int pos = 0, end = 0, share = 1, start;      // (the host sees to it that all groups fit 30 bits)
     PagedSeq first64{};
     int groups64 = 0, sum64 = 0;
     auto locate = [&](int at, PagedUnit &u, PagedSeq &s) {
@@ -814,9 +814,11 @@ __global__ __launch_bounds__(256, (NB * HD < 256 && PagedWave<CT, HD, NB>::kRing
             for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, kWave));
             share = max(share, __builtin_amdgcn_readfirstlane(most) / kParts + 1);
         }
-        pos = share * (int)blockIdx.x;
-        end = min(pos + share, total);
-        if (pos >= end || !locate(pos, u, s)) return;
+        const long from = (long)share * blockIdx.x;
+        if (from >= total) return;
+        pos = (int)from;
+        end = (int)min(from + share, (long)total);
+        if (!locate(pos, u, s)) return;
     } else {
         u.pair = (int)blockIdx.x / c.a.n_kv;
         u.h = (int)blockIdx.x % c.a.n_kv;
@@ -826,6 +828,7 @@ __global__ __launch_bounds__(256, (NB * HD < 256 && PagedWave<CT, HD, NB>::kRing
         s = paged_seq(c.a, u.pair / c.row_tiles);
     }
 
+    start = pos;
     for (;;) {
         const int h = u.h, pair = u.pair;
         const PagedTile t = paged_tile<kKeyTile>(c, s, pair % c.row_tiles, kRows);
@@ -890,7 +893,7 @@ __global__ __launch_bounds__(256, (NB * HD < 256 && PagedWave<CT, HD, NB>::kRing
         }
         __syncthreads();
         // a part's place: 2 to a workgroup, the first for the unit that its share begins with
-        const size_t place = 2 * (size_t)blockIdx.x + (pos == share * blockIdx.x ? 0 : 1);
+        const size_t place = 2 * (size_t)blockIdx.x + (pos == start ? 0 : 1);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             float M = -INFINITY;
