@@ -298,7 +298,8 @@ typedef struct {
  * The host says how much that is at most, which decides grids and workspaces: `rows` in all (exact),
  * max_q / min_q rows of one sequence and max_kv positions of one.  The arrays may change between calls (a
  * captured graph reads them anew); nothing is read or written out of range where they exceed the bounds, but
- * rows beyond max_q, and sequences with fewer than min_q, may then not be computed by ead_paged_attention.  Limits: batch <= 65535, rows * heads < 2^30. */
+ * rows beyond max_q, and sequences with fewer than min_q, may then not be computed by ead_paged_attention.
+ * Limits: batch <= 65535, rows * heads < 2^30. */
 typedef struct {
     int32_t batch, rows, max_q, min_q, max_kv, table_stride, table_width;
     const int32_t *page_table, *q_starts, *kv_lens;
@@ -324,7 +325,8 @@ ead_status ead_paged_read(const ead_paged_cache *cache, const ead_paged_batch *b
  * cache, EAD_BF16 over an EAD_BF16 or EAD_FP8 one.  Query head h reads KV head h / (n_heads / n_kv_heads).  The row
  * at position p sees positions j <= p, with window > 0 only those with p - j < window or j < sinks.
  *   out = sum_j softmax_j(scale q.k_j) v_j;  lse (nullable, [rows][n_heads] float32) = ln sum_j exp(scale q.k_j)
- * `out` does not overlap q or the pages.  A row that sees nothing gets 0 and -infinity.  What is not seen has no effect, whatever it holds (NaN too).
+ * `out` does not overlap q or the pages.  A row that sees nothing gets 0 and -infinity.  What is not seen has no
+ * effect, whatever it holds (NaN too).
  * Scores, statistics and sums are float32.  Over 16- and 8-bit pages probabilities enter their product as two bf16
  * terms (16 bits), as one in calls of many rows per KV head over more than 4096 keys except at the masks' edges.
  * n_heads / n_kv_heads is an integer from 1 to 64; scale is positive. */
@@ -332,8 +334,9 @@ typedef struct {
     int32_t n_heads, dtype, window, sinks;
     float scale;
 } ead_paged_attn;
-/* Bytes of device memory an attention call needs (0 possible).  The caller clears them once, before the first
- * call that gets them; every call leaves what the next one expects.  A workspace serves one stream at a time. */
+/* Bytes of device memory an attention call needs (0 possible), 16-byte aligned.  The caller clears them once, before
+ * the first call that gets them; every call leaves what the next one of the same cache layout, bounds of the batch
+ * and attn expects.  For others it is cleared again.  A workspace serves one stream at a time. */
 ead_status ead_paged_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch,
                                const ead_paged_attn *attn, uint64_t *bytes);
 ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_batch *batch,

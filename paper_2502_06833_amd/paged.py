@@ -68,6 +68,17 @@ def _rows(name, t, rows, heads, dim) -> Rows:
     return Rows(t.data_ptr(), s[0], s[1])
 
 
+def _empty_like(q):
+    """A dense tensor of q's shape and type (torch.empty with a device takes three times as long on the host)."""
+    import torch
+    return torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
+
+
+def _empty_f32(q, *shape):
+    import torch
+    return q.new_empty(shape, dtype=torch.float32)
+
+
 class PagedBatch:
     """What a step works on.  page_table [batch, width], q_starts [batch + 1] and kv_lens [batch] are int32 tensors on the GPU
     and stay the caller's: they may be changed in place between calls as long as the bounds hold."""
@@ -146,6 +157,7 @@ class PagedCache:
         self._desc = CacheDesc(self._code, n, self.page_size, self.n_kv_heads, self.head_dim, *ptr)
         self._ref = C.byref(self._desc)
         self._key = (self._code, self.page_size, self.n_kv_heads, self.head_dim)
+        self._attention = lib().ead_paged_attention
         self._scale = 1.0 / float(self.head_dim) ** 0.5
 
     @classmethod
@@ -171,9 +183,8 @@ class PagedCache:
         """(k, v) [rows, n_kv_heads, head_dim] of the batch's rows, as `dtype` (bfloat16 if not said) or into `out`."""
         import torch
         if out is None:
-            shape = (batch.rows, self.n_kv_heads, self.head_dim)
-            t = torch.bfloat16 if dtype is None else dtype
-            out = tuple(torch.empty(shape, dtype=t, device=self.k_pages.device) for _ in range(2))
+            k = self.k_pages.new_empty((batch.rows, self.n_kv_heads, self.head_dim), dtype=torch.bfloat16 if dtype is None else dtype)
+            out = (k, torch.empty_like(k))
         k, v = out
         if v.dtype != k.dtype:
             raise ValueError(f"out of one type is needed, got {k.dtype} and {v.dtype}")
@@ -188,22 +199,21 @@ class PagedCache:
         over a float32 cache, bfloat16 over the others.  A row sees the positions up to its own; with window > 0 the last
         `window` of them and the first `sinks` of the sequence.  scale: 1 / sqrt(head_dim) if not said.  want_lse: also the
         logarithm of the sum of exponentials, [rows, n_heads] float32.  Rows that see nothing get 0 and -inf."""
-        import torch
-        code = _code(q)
         if q.dim() != 3:
             raise ValueError(f"q: expected [rows, n_heads, {self.head_dim}], got {list(q.shape)}")
-        if code != (F32 if self._code == F32 else BF16):
+        if _code(q) != (F32 if self._code == F32 else BF16):
             raise ValueError(f"{q.dtype} queries over {self.k_pages.dtype} pages: float32 over float32, bfloat16 over the others")
-        n_heads = q.shape[1]
-        rq = _rows("q", q, batch.rows, n_heads, self.head_dim)
+        rows, n_heads, dim = batch.rows, q.shape[1], self.head_dim
+        rq = _rows("q", q, rows, n_heads, dim)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = _empty_like(q)
         elif out.dtype != q.dtype:
             raise ValueError(f"out: {q.dtype} is needed, got {out.dtype}")
-        ro = _rows("out", out, batch.rows, n_heads, self.head_dim)
-        lse = torch.empty((batch.rows, n_heads), dtype=torch.float32, device=q.device) if want_lse else None
+        ro = _rows("out", out, rows, n_heads, dim)
+        lse = _empty_f32(q, rows, n_heads) if want_lse else None
         stream = _stream_ptr()
         p = batch._plan(self, n_heads, window, sinks, self._scale if scale is None else scale, stream)
-        _check(lib().ead_paged_attention(self._ref, batch._ref, p[0], C.byref(rq), C.byref(ro),
-                                         lse.data_ptr() if want_lse else None, p[1], p[2], stream))
+        rc = self._attention(self._ref, batch._ref, p[0], C.byref(rq), C.byref(ro), lse.data_ptr() if want_lse else None, p[1], p[2], stream)
+        if rc:
+            _check(rc)
         return (out, lse) if want_lse else out
