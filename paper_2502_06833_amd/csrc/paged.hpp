@@ -260,25 +260,15 @@ __device__ __forceinline__ bool paged_sees(const PagedAttn &c, int pos, int key)
     return key <= pos && (!c.window || pos - key < c.window || key < c.sinks);
 }
 
-// N bytes of device memory as words; N = 2: the half word in the low bits
+// N bytes (a multiple of 16) of device memory as words
 template <int N> struct Raw {
-    static constexpr int kWords = N < 4 ? 1 : N / 4;
-    uint32_t w[kWords];
+    uint32_t w[N / 4];
     __device__ __forceinline__ void load(const void *p) {
-        if constexpr (N == 2) w[0] = *(gptr<uint16_t>)p;
-        else if constexpr (N == 4) w[0] = *(gptr<uint32_t>)p;
-        else if constexpr (N == 8) { typedef uint32_t u32x2_t __attribute__((ext_vector_type(2))); const u32x2_t x = *(gptr<u32x2_t>)p; w[0] = x.x; w[1] = x.y; }
-        else {
 #pragma unroll
-            for (int i = 0; i < N / 16; ++i) {
-                const u32x4_t x = ((gptr<u32x4_t>)p)[i];
-                w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-            }
+        for (int i = 0; i < N / 16; ++i) {
+            const u32x4_t x = ((gptr<u32x4_t>)p)[i];
+            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
         }
-    }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) w[i] = 0u;
     }
 };
 
