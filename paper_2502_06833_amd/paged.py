@@ -80,8 +80,9 @@ def _empty_f32(q, *shape):
 
 
 class PagedBatch:
-    """What a step works on.  page_table [batch, width], q_starts [batch + 1] and kv_lens [batch] are int32 tensors on the GPU
-    and stay the caller's: they may be changed in place between calls as long as the bounds hold."""
+    """What a step works on.  page_table [batch, width] (rows of its own for every sequence, not an expanded one), q_starts [batch + 1]
+    and kv_lens [batch] are int32 tensors on the GPU and stay the caller's: they may be changed in place between calls as long as the
+    bounds hold."""
 
     def __init__(self, page_table, q_starts, kv_lens, *, rows, max_q, max_kv, min_q=0):
         import torch
@@ -93,11 +94,13 @@ class PagedBatch:
             raise ValueError(f"{n} sequences in page_table need q_starts of {n + 1} and kv_lens of {n}")
         if page_table.device != q_starts.device or page_table.device != kv_lens.device:
             raise ValueError("page_table, q_starts and kv_lens have to be on one device")
+        width = page_table.shape[1]
+        stride = page_table.stride(0) if n > 1 else width         # a single row's stride says nothing
+        if stride < width:
+            raise ValueError("page_table: its rows overlap (an expanded table?); .contiguous() gives every sequence its own")
         self.page_table, self.q_starts, self.kv_lens = page_table, q_starts, kv_lens
         self.rows = rows
-        width = page_table.shape[1]
-        self._desc = BatchDesc(n, rows, max_q, min_q, max_kv, max(page_table.stride(0), width), width, page_table.data_ptr(),
-                               q_starts.data_ptr(), kv_lens.data_ptr())
+        self._desc = BatchDesc(n, rows, max_q, min_q, max_kv, stride, width, page_table.data_ptr(), q_starts.data_ptr(), kv_lens.data_ptr())
         self._ref = C.byref(self._desc)
         self._plans = {}
 

@@ -1,0 +1,45 @@
+"""What PagedBatch and PagedCache make of their tensors, without a GPU: stand-ins say that they lie on one."""
+import pytest
+import torch
+
+import paper_2502_06833_amd as ead
+
+
+class OnGpu:
+    """A CPU tensor that says it is on a GPU: for checks and descriptors, which never touch the data."""
+
+    def __init__(self, t, device="cuda:0"):
+        self.t, self.device, self.is_cuda = t, torch.device(device), True
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def batch_of(page_table, device="cuda:0", **kw):
+    n = page_table.shape[0]
+    lens = torch.zeros(n, dtype=torch.int32)
+    bounds = dict(rows=n, max_q=1, max_kv=1)
+    bounds.update(kw)
+    return ead.PagedBatch(OnGpu(page_table, device), OnGpu(torch.zeros(n + 1, dtype=torch.int32), device), OnGpu(lens, device), **bounds)
+
+
+def test_overlapping_rows_of_a_page_table_are_refused():
+    """An expanded row has a stride of 0: taken for rows `width` apart, sequence b's would be looked for b * width entries past its end."""
+    row = torch.arange(4, dtype=torch.int32)[None]
+    with pytest.raises(ValueError):
+        batch_of(row.expand(3, -1))
+    with pytest.raises(ValueError):
+        batch_of(torch.arange(16, dtype=torch.int32).as_strided((3, 4), (2, 1)))
+    assert batch_of(row.expand(3, -1).contiguous())._desc.table_stride == 4
+
+
+def test_strides_of_page_tables():
+    wide = torch.arange(40, dtype=torch.int32).view(4, 10)
+    d = batch_of(wide[:, :6])._desc                          # columns of a wider table
+    assert (d.table_width, d.table_stride) == (6, 10)
+    d = batch_of(wide[::2, 2:])._desc                        # every second row
+    assert (d.table_width, d.table_stride) == (8, 20)
+    d = batch_of(wide[:1].expand(1, -1))._desc               # one sequence: its stride says nothing
+    assert d.table_width == 10 and d.table_stride >= 10
+    d = batch_of(torch.arange(3, dtype=torch.int32).as_strided((1, 3), (0, 1)))._desc
+    assert d.table_width == 3 and d.table_stride >= 3
