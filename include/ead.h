@@ -291,7 +291,8 @@ typedef struct {
 /* What a call works on: `batch` sequences, each with some rows (its new tokens).  Arrays are device memory.
  *   page_table [batch][table_stride], the first table_width entries of a row are used: entry i is the
  *              page of positions i * page_size .. + page_size.  A number outside 0 .. n_pages-1 is a hole:
- *              nothing is written there, zeros are read from there, and attention sees nothing there
+ *              nothing is written there, zeros are read from there, and attention sees nothing there.
+ *              Positions past the last entry are holes too
  *   q_starts   [batch + 1]: rows q_starts[b] .. q_starts[b+1]-1 of the call's tensors are sequence b's
  *   kv_lens    [batch]: positions the sequence holds, its rows the last of them (row i of n is position
  *              kv_lens[b] - n + i; rows at positions below 0 are neither written nor see anything)

@@ -175,11 +175,8 @@ struct PagedCall {
     PagedPlan m;
     uint64_t f_bytes, m_bytes;
 };
-PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_paged_attn *given) {
+PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_paged_attn *at) {
     const long capacity = (long)b->table_width * c->page_size;
-    ead_paged_attn seen = *given;
-    if (seen.window >= capacity) seen.window = 0;            // every position is in it
-    const ead_paged_attn *at = &seen;
     const int held = (int)std::min((long)b->max_kv, capacity), group = at->n_heads / c->n_kv_heads, cus = compute_units();
     const bool f32 = c->dtype == EAD_F32;
     const long rows = (long)b->max_q * group;
@@ -252,7 +249,7 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     c.n_heads = attn->n_heads;
     c.group = attn->n_heads / cache->n_kv_heads;
     c.c2 = attn->scale * 1.4426950408889634f;
-    c.window = attn->window >= (long)batch->table_width * cache->page_size ? 0 : attn->window;
+    c.window = attn->window;
     c.sinks = attn->sinks;
     c.few_rows = p.few_rows;
     const hipStream_t st = (hipStream_t)hip_stream;

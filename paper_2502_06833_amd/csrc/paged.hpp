@@ -22,31 +22,28 @@ struct PagedArgs {
     int table_stride, table_width, rows;
 };
 
-// A sequence as the device arrays have it, cut to what the host vouched for: row0 + n_rows <= rows, 0 <= kv <= table.
+// A sequence as the device arrays have it, cut to what the host vouched for: row0 + n_rows <= rows, 0 <= kv <= table.  Rows keep the positions that the
+// uncut length gives them: where a table ends before its sequence, what lies past it are holes.
 struct PagedSeq {
-    int row0, n_rows, kv, first;                  // first: position of its first row (below 0 where kv < n_rows)
+    int row0, n_rows, kv, first;                  // kv: positions that the table reaches; first: position of its first row (below 0 where it has more rows than positions)
     const int *table;
 };
-__device__ __forceinline__ PagedSeq paged_seq(const PagedArgs &a, int b) {
+__device__ __forceinline__ PagedSeq paged_seq_of(const PagedArgs &a, int start, int end, int len, const int *table) {
     PagedSeq s;
-    // (b is the workgroup's: the readfirstlanes say so, which keeps what follows from these in scalar registers)
-    s.row0 = min(max(__builtin_amdgcn_readfirstlane(a.q_starts[b]), 0), a.rows);
-    s.n_rows = min(max(__builtin_amdgcn_readfirstlane(a.q_starts[b + 1]), s.row0), a.rows) - s.row0;
-    s.kv = min(max(__builtin_amdgcn_readfirstlane(a.kv_lens[b]), 0), (int)min((long)a.table_width << a.page_shift, (long)0x7FFFFF00));
-    s.first = s.kv - s.n_rows;
-    s.table = a.table + (size_t)b * a.table_stride;
+    s.row0 = min(max(start, 0), a.rows);
+    s.n_rows = min(max(end, s.row0), a.rows) - s.row0;
+    s.kv = min(max(len, 0), (int)min((long)a.table_width << a.page_shift, (long)0x7FFFFF00));
+    s.first = max(len, 0) - s.n_rows;
+    s.table = table;
     return s;
+}
+__device__ __forceinline__ PagedSeq paged_seq(const PagedArgs &a, int b) {
+    // (b is the workgroup's: the readfirstlanes say so, which keeps what follows from these in scalar registers)
+    return paged_seq_of(a, __builtin_amdgcn_readfirstlane(a.q_starts[b]), __builtin_amdgcn_readfirstlane(a.q_starts[b + 1]), __builtin_amdgcn_readfirstlane(a.kv_lens[b]),
+                        a.table + (size_t)b * a.table_stride);
 }
 // the same for a number that differs from lane to lane
-__device__ __forceinline__ PagedSeq paged_seq_lane(const PagedArgs &a, int b) {
-    PagedSeq s;
-    s.row0 = min(max(a.q_starts[b], 0), a.rows);
-    s.n_rows = min(max(a.q_starts[b + 1], s.row0), a.rows) - s.row0;
-    s.kv = min(max(a.kv_lens[b], 0), (int)min((long)a.table_width << a.page_shift, (long)0x7FFFFF00));
-    s.first = s.kv - s.n_rows;
-    s.table = nullptr;
-    return s;
-}
+__device__ __forceinline__ PagedSeq paged_seq_lane(const PagedArgs &a, int b) { return paged_seq_of(a, a.q_starts[b], a.q_starts[b + 1], a.kv_lens[b], nullptr); }
 // The page of a position 0 <= pos < kv; -1: a hole
 __device__ __forceinline__ int paged_page(const PagedArgs &a, const PagedSeq &s, int pos) {
     const int id = s.table[pos >> a.page_shift];
@@ -153,7 +150,7 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedCopy c) {
     const int lane = (int)threadIdx.x % L;
     for (int i = (int)blockIdx.x * kVecs + (int)threadIdx.x / L; i < total; i += (int)gridDim.x * kVecs) {
         const int t = i / c.a.n_kv, h = i % c.a.n_kv, pos = s.first + t;
-        bool live = pos >= 0;
+        bool live = pos >= 0 && pos < s.kv;
         float fk[8] = {}, fv[8] = {};
         size_t vec = 0;
         if (live) {
@@ -206,7 +203,7 @@ __global__ __launch_bounds__(256) void k_paged_read(PagedCopy c) {
     const int lane = (int)threadIdx.x % L;
     for (int i = (int)blockIdx.x * kVecs + (int)threadIdx.x / L; i < total; i += (int)gridDim.x * kVecs) {
         const int t = i / c.a.n_kv, h = i % c.a.n_kv, pos = s.first + t;
-        const int page = pos >= 0 ? paged_page(c.a, s, pos) : -1;
+        const int page = pos >= 0 && pos < s.kv ? paged_page(c.a, s, pos) : -1;
         float fk[8] = {}, fv[8] = {};
         if (page >= 0) {
             const size_t vec = paged_vec(c.a, page, h, pos & ((1 << c.a.page_shift) - 1));
@@ -253,7 +250,7 @@ __device__ __forceinline__ PagedTile paged_tile(const PagedAttn &c, const PagedS
     t.p_hi = s.first + (t.r0 + max(t.rows, 1) - 1) / c.group;
     t.t_lo = c.window ? max(0, max(t.p_lo, 0) - c.window + 1) / KEYS : 0;
     t.n_sink = c.window ? min((min(c.sinks, s.kv) + KEYS - 1) / KEYS, t.t_lo) : 0;
-    t.tiles = t.rows > 0 && t.p_hi >= 0 ? t.n_sink + max(t.p_hi / KEYS + 1 - t.t_lo, 0) : 0;
+    t.tiles = t.rows > 0 && t.p_hi >= 0 ? t.n_sink + max(min(t.p_hi, s.kv - 1) / KEYS + 1 - t.t_lo, 0) : 0;
     return t;
 }
 __device__ __forceinline__ bool paged_sees(const PagedAttn &c, int pos, int key) {
@@ -775,7 +772,7 @@ __global__ __launch_bounds__(256, (NB * HD < 256 && PagedWave<CT, HD, NB>::kRing
                 s.row0 = __builtin_amdgcn_readlane(x.row0, i);
                 s.n_rows = __builtin_amdgcn_readlane(x.n_rows, i);
                 s.kv = __builtin_amdgcn_readlane(x.kv, i);
-                s.first = s.kv - s.n_rows;
+                s.first = __builtin_amdgcn_readlane(x.first, i);
                 s.table = c.a.table + (size_t)(u.pair / c.row_tiles) * c.a.table_stride;
                 return true;
             }

@@ -1,0 +1,71 @@
+"""The paged cache where calls leave the ordinary: tables that end before their sequences, workspaces and graphs, infinities and
+magnitudes at the ends of their types.  Definitions, tolerances and set-ups are those of test_gpu_paged.py."""
+import pytest
+import torch
+
+import paper_2502_06833_amd as ead
+from test_gpu_paged import DEV, F8, TYPES, Setup, check_attention, exact_attention, way  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# (rows, positions, pages that the table has of 16 positions each)
+SHORT = [(1, 33, 2), (1, 300, 2), (7, 36, 2), (5, 200, 12), (40, 70, 3), (150, 400, 20), (150, 180, 1)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("q_len,kv,width", SHORT)
+def test_positions_past_the_table_are_holes(way, dtype, q_len, kv, width):
+    """A table that ends before its sequence: the rest are holes.  Rows stay at their positions: nothing is written over others', nothing is
+    read there, and what a row sees goes by its own position."""
+    s = Setup([q_len, 2], [kv, 9], 2, 64, dtype, 16, seed=kv)
+    s.write_all()
+    short = ead.PagedBatch.of(s.table[:, :width], [q_len, 2], [kv, 9])
+    past = [(0, p) for p in range(width, -(-kv // 16))]
+    q = s.queries(6)
+    for window, sinks in ((0, 0), (16 * width, 0), (16 * width + 1, 4), (20, 3), (3, 0), (2 ** 31 - 1, 2 ** 31 - 1)):
+        got, lse = s.cache.attention(q, short, window=window, sinks=sinks, want_lse=True)
+        check_attention(s, q, got, lse, exact_attention(s, q, window, sinks, holes=past))
+    first = kv - q_len
+    inside = torch.tensor([p < 16 * width for p in range(first, kv)] + [True, True], device=DEV)
+    k, v = s.cache.read(short, torch.float32)
+    whole = s.cache.read(s.batch, torch.float32)
+    for part, all_ in zip((k, v), whole):
+        assert bool((part[~inside] == 0).all()) and torch.equal(part[inside], all_[inside])
+    # written: what is inside, and nothing else
+    copies = [t.clone() if t is not None else None for t in (s.cache.k_pages, s.cache.v_pages, s.cache.k_scales, s.cache.v_scales)]
+    full = ead.PagedCache(*copies)
+    x = torch.randn(q_len + 2, 2, 64, generator=s.g, device=DEV)
+    full.write(x, -x, s.batch)
+    outside = s.table[0, width:].long()
+    outside = outside[outside >= 0]
+    for name in ("k_pages", "v_pages", "k_scales", "v_scales"):
+        have, want = getattr(s.cache, name), getattr(full, name)
+        if have is not None:
+            want.view(torch.uint8)[outside] = have.view(torch.uint8)[outside]
+    s.cache.write(x, -x, short)
+    for name in ("k_pages", "v_pages", "k_scales", "v_scales"):
+        if getattr(full, name) is not None:
+            assert torch.equal(getattr(s.cache, name).view(torch.uint8), getattr(full, name).view(torch.uint8)), name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("way_past", [2 ** 31 - 1, 2 ** 31 - 256, 10 ** 9])
+def test_lengths_far_past_the_table(way, dtype, way_past):
+    """Lengths up to the largest a device array holds: everything that the table has is seen, and nothing is written."""
+    s = Setup([3], [48], 2, 32, dtype, 16, seed=1)
+    s.write_all()
+    lens = torch.tensor([way_past], dtype=torch.int32, device=DEV)
+    far = ead.PagedBatch(s.table[:, :3], s.batch.q_starts, lens, rows=3, max_q=3, max_kv=way_past)
+    q = s.queries(4)
+    got, lse = s.cache.attention(q, far, want_lse=True)
+    s.kv_lens = [51]                                          # three rows past the 48 positions see them all
+    s.k, s.v = ([torch.cat([t[0], torch.zeros_like(t[0][:3])])] for t in (s.k, s.v))
+    check_attention(s, q, got, lse, exact_attention(s, q, holes=[(0, 3)]))
+    got, lse = s.cache.attention(q, far, window=40, sinks=5, want_lse=True)
+    check_attention(s, q, got, lse, exact_attention(s, q, 1, 5, holes=[(0, 3)]))
+    before = s.cache.k_pages.view(torch.uint8).clone()
+    x = torch.ones(3, 2, 32, device=DEV)
+    s.cache.write(x, x, far)
+    assert torch.equal(s.cache.k_pages.view(torch.uint8), before)
+    assert bool((s.cache.read(far)[0] == 0).all())
