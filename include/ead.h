@@ -337,7 +337,9 @@ typedef struct {
 } ead_paged_attn;
 /* Bytes of device memory an attention call needs (0 possible), 16-byte aligned.  The caller clears them once, before
  * the first call that gets them; every call leaves what the next one of the same cache layout, bounds of the batch
- * and attn expects.  For others it is cleared again.  A workspace serves one stream at a time. */
+ * and attn expects.  For others it is cleared again.  A workspace serves one stream at a time; one that captured calls
+ * get is their graph's (cleared, by a kernel, in the graph or before its first replay): a graph that runs beside other
+ * calls shares none with them. */
 ead_status ead_paged_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch,
                                const ead_paged_attn *attn, uint64_t *bytes);
 ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_batch *batch,

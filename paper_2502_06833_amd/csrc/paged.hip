@@ -274,6 +274,16 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     return launched("ead_paged_attention");
 }
 
+// For the Python classes, in no header: the number of the capture that a stream is in, 0 where nothing is captured
+ead_status ead_stream_capture(void *hip_stream, uint64_t *id) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    unsigned long long n = 0;
+    const hipError_t e = hipStreamGetCaptureInfo((hipStream_t)hip_stream, &status, &n);
+    if (e != hipSuccess) return refuse(EAD_ERR_DEVICE, "hipStreamGetCaptureInfo: %s", hipGetErrorString(e));
+    *id = status == hipStreamCaptureStatusActive ? n : 0;
+    return EAD_OK;
+}
+
 // For the tests alone, in no header: the work up to which one kernel takes a call alone (-1: as ever), and whether units are always cut into shares.
 ead_status ead_test_paged(double small_work, int32_t always_shares) {
     g_small_work = small_work < 0 ? kPagedSmallWork : small_work;

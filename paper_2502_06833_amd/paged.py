@@ -79,10 +79,22 @@ def _empty_f32(q, *shape):
     return q.new_empty(shape, dtype=torch.float32)
 
 
+def _capturing():
+    """Whether the current stream is being captured (torch's accessor, looked up once)."""
+    global _capturing
+    import torch
+    _capturing = torch.cuda.is_current_stream_capturing
+    return _capturing()
+
+
 class PagedBatch:
     """What a step works on.  page_table [batch, width] (rows of its own for every sequence, not an expanded one), q_starts [batch + 1]
     and kv_lens [batch] are int32 tensors on the GPU and stay the caller's: they may be changed in place between calls as long as the
-    bounds hold."""
+    bounds hold.
+
+    A batch keeps the workspaces of `PagedCache.attention`, one for each stream.  Calls under a graph capture get one that belongs to the
+    graph: it lies in the graph's memory and a node of the graph clears it, so captures need no call before them, and graphs of one batch
+    may run beside each other and beside eager calls."""
 
     def __init__(self, page_table, q_starts, kv_lens, *, rows, max_q, max_kv, min_q=0):
         import torch
@@ -103,6 +115,7 @@ class PagedBatch:
         self._desc = BatchDesc(n, rows, max_q, min_q, max_kv, stride, width, page_table.data_ptr(), q_starts.data_ptr(), kv_lens.data_ptr())
         self._ref = C.byref(self._desc)
         self._plans = {}
+        self._of_capture = (0, {})
 
     @classmethod
     def of(cls, page_table, q_lens, kv_lens):
@@ -121,17 +134,26 @@ class PagedBatch:
         return cls(page_table, torch.tensor(starts, dtype=torch.int32).to(dev), torch.tensor(kv_lens, dtype=torch.int32).to(dev),
                    rows=starts[-1], max_q=max(q_lens, default=0), min_q=min(q_lens, default=0), max_kv=max(kv_lens, default=0))
 
+    def _captured_plans(self, stream):
+        """The plans of the capture under way: they go with the next one, and their memory is the graph's until then and after."""
+        n = C.c_uint64(0)
+        _check(lib().ead_stream_capture(C.c_void_p(stream), C.byref(n)))
+        if self._of_capture[0] != n.value:
+            self._of_capture = (n.value, {})
+        return self._of_capture[1]
+
     def _plan(self, cache, n_heads, window, sinks, scale, stream):
         """The attention arguments, and the workspace of this stream: cleared once, then every call leaves it ready for the next."""
+        plans = self._captured_plans(stream) if _capturing() else self._plans
         key = (stream, cache._key, n_heads, window, sinks, scale)
-        p = self._plans.get(key)
+        p = plans.get(key)
         if p is None:
             import torch
             d = AttnDesc(n_heads, F32 if cache._code == F32 else BF16, window, sinks, scale)
             need = C.c_uint64(0)
             _check(lib().ead_paged_workspace(cache._ref, self._ref, C.byref(d), C.byref(need)))
             ws = torch.zeros((need.value + 3) // 4, dtype=torch.int32, device=self.kv_lens.device) if need.value else None
-            p = self._plans[key] = (C.byref(d), ws.data_ptr() if need.value else None, need.value, d, ws)
+            p = plans[key] = (C.byref(d), ws.data_ptr() if need.value else None, need.value, d, ws)
         return p
 
 

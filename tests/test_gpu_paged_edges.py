@@ -69,3 +69,108 @@ def test_lengths_far_past_the_table(way, dtype, way_past):
     s.cache.write(x, x, far)
     assert torch.equal(s.cache.k_pages.view(torch.uint8), before)
     assert bool((s.cache.read(far)[0] == 0).all())
+
+
+# ---- graphs
+def _soiled_pool():
+    """A graph pool whose free memory holds no zeros, and the graph that it belongs to."""
+    pool, g = torch.cuda.graph_pool_handle(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, pool=pool):
+        used = [torch.full((n,), 0x01010101, dtype=torch.int32, device=DEV) for n in [1 << 15] * 8 + [1 << 24] * 2]
+    g.replay()
+    torch.cuda.synchronize()
+    del used
+    return pool, g
+
+
+def _captured(s, q, outs, pool=None):
+    """A graph of one attention call for each of outs, on torch's own capture stream."""
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, pool=pool):
+        for out in outs:
+            s.cache.attention(q, s.batch, out=out)
+    return g
+
+
+@pytest.mark.parametrize("lens", [([1], [6000]), ([300], [5000])])
+def test_first_calls_under_capture(way, lens):
+    """No eager call before, two graphs of one batch on one capture stream, the second replayed first, then eager calls there and elsewhere:
+    every one finds a workspace that was cleared for it."""
+    def fresh():
+        s = Setup(*lens, 1, 128, torch.bfloat16, 16, seed=5)
+        s.write_all()
+        return s, s.queries(8)
+
+    s, q = fresh()
+    want = s.cache.attention(q, s.batch)
+    s, q = fresh()                                            # the same values, a batch that nothing was called for
+    outs = [torch.full_like(q, 9.0) for _ in range(4)]
+    (pool, zeroth), (pool2, zeroth2) = _soiled_pool(), _soiled_pool()
+    first, second = _captured(s, q, outs[:2], pool), _captured(s, q, outs[2:], pool2)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for graph, mine in ((second, outs[2:]), (first, outs[:2])):
+            for o in outs:
+                o.fill_(9.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            for o in mine:
+                assert torch.equal(o, want)
+            assert torch.equal(s.cache.attention(q, s.batch), want)
+    s2, q2 = fresh()
+    out = torch.full_like(q2, 9.0)
+    pool, zeroth = _soiled_pool()
+    graph = _captured(s2, q2, [out], pool)
+    with torch.cuda.stream(torch.cuda.graph.default_capture_stream):           # eager on the capture stream, before any replay
+        assert torch.equal(s2.cache.attention(q2, s2.batch), want)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_graphs_of_one_batch_replayed_side_by_side(way):
+    """Graphs captured on one stream and replayed on others at the same time, beside eager calls on the capture stream."""
+    s = Setup([1], [30000], 2, 128, torch.bfloat16, 16, seed=6)
+    s.write_all()
+    qs = [s.queries(16) for _ in range(3)]
+    want = [s.cache.attention(q, s.batch) for q in qs]
+    with torch.cuda.stream(torch.cuda.graph.default_capture_stream or torch.cuda.Stream()):
+        s.cache.attention(qs[2], s.batch)
+    outs = [[torch.zeros_like(q) for _ in range(4)] for q in qs[:2]]
+    graphs = [_captured(s, q, o) for q, o in zip(qs, outs)]
+    streams = [torch.cuda.Stream() for _ in graphs]
+    torch.cuda.synchronize()
+    for _ in range(50):
+        eager = []
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        with torch.cuda.stream(torch.cuda.graph.default_capture_stream):
+            for _ in range(4):
+                eager.append(s.cache.attention(qs[2], s.batch))
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            for x in o:
+                assert torch.equal(x, w)
+                x.zero_()
+        assert all(torch.equal(x, want[2]) for x in eager)
+        torch.cuda.synchronize()
+
+
+def test_a_graph_keeps_its_workspace(way):
+    """The batch goes, the graph stays: its workspace lies in the graph's own memory."""
+    s = Setup([1], [6000], 1, 128, torch.bfloat16, 16, seed=5)
+    s.write_all()
+    q = s.queries(8)
+    want = s.cache.attention(q, s.batch)
+    out = torch.zeros_like(q)
+    graph = _captured(s, q, [out])
+    lengths = s.batch.q_starts, s.batch.kv_lens               # these are the caller's to keep
+    s.batch = None
+    junk = [torch.full((1 << 22,), 0x01010101, dtype=torch.int32, device=DEV) for _ in range(20)]
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    assert all(bool((t == 0x01010101).all()) for t in junk) and len(lengths) == 2
