@@ -649,8 +649,8 @@ __device__ __forceinline__ bool paged_last(const PagedAttn &c, size_t unit, int 
 
 // The parts of a unit joined, part i of `used` at place_of(i): their order is that of the key ranges, whoever arrived last.
 // A part is tile_rows * HD / 4 vectors of four outputs, of which the first `items` are looked at; where(e) says which row and outputs vector e is.  `table`: LDS for used * tile_rows maxima and
-// sums.  A thread has FLIGHT vectors on their way at a time, P parts of FLIGHT / P of its own (the last part again where there are fewer than P): this
-// is one workgroup's work while others may be done, and latency is what it costs.
+// sums.  A thread has FLIGHT vectors on their way at a time, P parts of FLIGHT / P of its own (the last part again where there are fewer than
+// P, then taken as zeros: a weight of 0 would make NaN of its infinities): this is one workgroup's work while others may be done, and latency is what it costs.
 struct PagedWhere { int row, d; };
 template <typename OT, int HD, int P, int FLIGHT, bool PAST, typename F, typename G>
 __device__ __forceinline__ void paged_join_by(const PagedAttn &c, const PagedSeq &s, const PagedTile &t, int h, int used, int items, size_t part_vecs, const float2 *table, F place_of, G where) {
@@ -685,7 +685,7 @@ __device__ __forceinline__ void paged_join_by(const PagedAttn &c, const PagedSeq
                     const float2 y = table[min(i0 + i, used - 1) * t.rows + row];
                     const float f = i0 + i < used ? __builtin_amdgcn_exp2f(y.x - ref) : 0.f;
                     L[k] += f * y.y;
-                    v[k] += f * x[k][i];
+                    v[k] += f * (i0 + i < used ? x[k][i] : f32x4e_t{0.f, 0.f, 0.f, 0.f});
                 }
             }
         }

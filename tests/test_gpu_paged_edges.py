@@ -174,3 +174,45 @@ def test_a_graph_keeps_its_workspace(way):
         torch.cuda.synchronize()
         assert torch.equal(out, want)
     assert all(bool((t == 0x01010101).all()) for t in junk) and len(lengths) == 2
+
+
+# ---- infinities
+def check_infinities(s, q, at, window=0, sinks=0):
+    """V with an infinity in dimension 10 of position at[0] of every sequence, one of the other sign in 11, and both in 12 at at[0] and at[1]: a
+    row that sees it has that infinity (NaN: both) there, whatever its weight, and everything else is as ever."""
+    k, v = ([t.float().clone() for t in x] for x in (s.k, s.v))
+    for x in v:
+        for p in at:
+            x[p, :, 10], x[p, :, 11] = torch.inf, -torch.inf
+        x[at[0], :, 12], x[at[-1], :, 12] = torch.inf, -torch.inf if len(at) > 1 else torch.inf
+    s.write_all(k=torch.cat(k), v=torch.cat(v))
+    got, lse = s.cache.attention(q, s.batch, window=window, sinks=sinks, want_lse=True)
+    s.v = [torch.where(torch.isfinite(x), x, 0.0) for x in s.v]
+    out, z, mass = exact_attention(s, q, window, sinks)
+    pos = torch.cat([torch.arange(kv - ql, kv, device=DEV) for ql, kv in zip(s.q_lens, s.kv_lens)])
+
+    def sees(p):
+        return (p <= pos) & ((pos - p < window) | (p < sinks) if window else pos >= 0)
+
+    any_, first, last = torch.stack([sees(p) for p in at]).any(0), sees(at[0]), sees(at[-1])
+    want = out.clone()
+    want[any_, :, 10], want[any_, :, 11] = torch.inf, -torch.inf
+    if len(at) == 1:
+        want[first, :, 12] = torch.inf
+    else:
+        want[first & ~last, :, 12], want[last & ~first, :, 12], want[first & last, :, 12] = torch.inf, -torch.inf, torch.nan
+    for d in (10, 11, 12):
+        assert torch.equal(torch.nan_to_num(got[:, :, d].double(), 9e9, 8e8, 7e7) >= 7e7, torch.nan_to_num(want[:, :, d], 9e9, 8e8, 7e7) >= 7e7), d
+        assert torch.equal(torch.isnan(got[:, :, d]), torch.isnan(want[:, :, d])) and torch.equal(torch.isinf(got[:, :, d]), torch.isinf(want[:, :, d]))
+    fine = torch.isfinite(want)
+    check_attention(s, q, torch.where(fine, got, 0.0), lse, (torch.where(fine, out, 0.0), z, mass))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("kv", [260, 390, 520, 650, 1300, 2100, 3400, 8190])
+def test_an_infinity_outlives_the_join_of_parts(way, dtype, hd, kv):
+    """The last position's, in a tile at the mask's edge: parts that are not there (their number is rounded up where they are read) add nothing."""
+    s = Setup([1], [kv], 2, hd, dtype, 16, seed=kv)
+    s.write_all()
+    check_infinities(s, s.queries(4), [kv - 1])
