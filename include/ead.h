@@ -327,7 +327,8 @@ ead_status ead_paged_read(const ead_paged_cache *cache, const ead_paged_batch *b
  * at position p sees positions j <= p, with window > 0 only those with p - j < window or j < sinks.
  *   out = sum_j softmax_j(scale q.k_j) v_j;  lse (nullable, [rows][n_heads] float32) = ln sum_j exp(scale q.k_j)
  * `out` does not overlap q or the pages.  A row that sees nothing gets 0 and -infinity.  What is not seen has no
- * effect, whatever it holds (NaN too).
+ * effect, whatever it holds (NaN too).  An infinity among the values that a row sees is its output there, and NaN where
+ * another opposes it or its probability is 0 in float32.
  * Scores, statistics and sums are float32.  Over 16- and 8-bit pages probabilities enter their product as two bf16
  * terms (16 bits), as one in calls of many rows per KV head over more than 4096 keys except at the masks' edges.
  * n_heads / n_kv_heads is an integer from 1 to 64; scale is positive. */

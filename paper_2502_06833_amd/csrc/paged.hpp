@@ -235,6 +235,14 @@ struct PagedAttn {
 
 constexpr int kKeyTile = 32;
 
+// Two bf16 terms of probabilities: the upper halves of their words, and what those leave, rounded (16 bits in all).  The rest gets 2^-22 of the probability on top
+// and is never 0 where that is not: times an infinity of V both terms are that infinity, where a rest of 0 or of the other sign would make it NaN.
+__device__ __forceinline__ uint32_t upper_bf16(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+__device__ __forceinline__ uint32_t rest_bf16(float a, float b) {
+    auto rest = [](float p) { return __builtin_fmaf(p, 1.f + 0x1p-22f, -__uint_as_float(__float_as_uint(p) & 0xFFFF0000u)); };
+    return pack_bf16(rest(a), rest(b));
+}
+
 // What a tile of rows sees.  Rows of a KV head are (token, head of the group) pairs, token first: row = token * group + head.
 struct PagedTile {
     int r0, rows;                   // first row, rows in the tile (0: none)
@@ -519,10 +527,12 @@ struct PagedWave {
             // two bf16 terms of every probability
             u32x4_t hi[NB], lo[NB];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                hi[b] = __builtin_bit_cast(u32x4_t, take_bf16(p[b]));
-                lo[b] = u32x4_t{pack_bf16(p[b][0], p[b][1]), pack_bf16(p[b][2], p[b][3]), pack_bf16(p[b][4], p[b][5]), pack_bf16(p[b][6], p[b][7])};
-            }
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    hi[b][e] = upper_bf16(p[b][2 * e], p[b][2 * e + 1]);
+                    lo[b][e] = rest_bf16(p[b][2 * e], p[b][2 * e + 1]);
+                }
 #pragma unroll
             for (int i = 0; i < HD / 16; ++i) {
                 u32x4_t v;

@@ -208,8 +208,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
                 for (int e = 0; e < 8; ++e) {
                     const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e], c.c2, -ref)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * e + 1], c.c2, -ref));
                     l += x + y;
-                    p[b][e] = pack_bf16(x, y);
-                    p_lo[b][e] = pack_bf16(x - __uint_as_float(p[b][e] << 16), y - __uint_as_float(p[b][e] & 0xFFFF0000u));
+                    p[b][e] = upper_bf16(x, y);
+                    p_lo[b][e] = rest_bf16(x, y);
                 }
 #pragma unroll
             for (int j = 0; j < 4; ++j)

@@ -216,3 +216,24 @@ def test_an_infinity_outlives_the_join_of_parts(way, dtype, hd, kv):
     s = Setup([1], [kv], 2, hd, dtype, 16, seed=kv)
     s.write_all()
     check_infinities(s, s.queries(4), [kv - 1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads", [(4, 2, 32), (6, 1, 128)])
+@pytest.mark.parametrize("at", [[3], [97], [40, 90], [7, 97]])
+@pytest.mark.parametrize("q_lens,kv_lens,window,sinks", [
+    ([1, 1], [700, 131], 0, 0), ([1], [3000], 0, 0), ([5, 3], [700, 100], 0, 0), ([200], [700], 0, 0), ([200, 1], [200, 1500], 0, 0),
+    ([1, 9], [150, 300], 100, 8), ([200, 60], [330, 300], 70, 60),
+])
+def test_infinities_that_rows_see(way, dtype, heads, at, q_lens, kv_lens, window, sinks):
+    """In tiles that every row sees whole as at the edges."""
+    n_heads, n_kv, hd = heads
+    s = Setup(q_lens, kv_lens, n_kv, hd, dtype, 16, seed=at[0])
+    s.write_all()
+    check_infinities(s, s.queries(n_heads), at, window, sinks)
+
+
+def test_infinities_in_long_contexts(way):
+    s = Setup([200, 1], [4800, 5000], 1, 64, torch.bfloat16, 64, seed=2)
+    s.write_all()
+    check_infinities(s, s.queries(4), [3, 2000])
