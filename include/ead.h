@@ -329,7 +329,9 @@ ead_status ead_paged_read(const ead_paged_cache *cache, const ead_paged_batch *b
  * `out` does not overlap q or the pages.  A row that sees nothing gets 0 and -infinity.  What is not seen has no
  * effect, whatever it holds (NaN too).  An infinity among the values that a row sees is its output there, and NaN where
  * another opposes it or its probability is 0 in float32.
- * Scores, statistics and sums are float32.  Over 16- and 8-bit pages probabilities enter their product as two bf16
+ * Scores, statistics and sums are float32; sums are divided by that of the exponentials at the end, and values within
+ * some powers of two of the largest float may overflow in them.  8-bit vectors of V whose power of two is below 2^-90
+ * lose bits (errors of up to 2^-100).  Over 16- and 8-bit pages probabilities enter their product as two bf16
  * terms (16 bits), as one in calls of many rows per KV head over more than 4096 keys except at the masks' edges.
  * n_heads / n_kv_heads is an integer from 1 to 64; scale is positive. */
 typedef struct {

@@ -326,6 +326,7 @@ struct PagedWave {
     static constexpr int VW = HD / 16 < 4 ? HD / 16 : 4;                     // float: neighbouring elements of V in one read
     static constexpr int KE = F32 ? 4 : F8 ? (HD >= 64 ? 16 : 8) : 8;        // neighbouring elements of K in one read
     static constexpr int KL = HD / 4 / KE;                                   // reads per key
+    static constexpr int kCodeBits = 9;                                      // 8 bits: V's codes are taken times 2^kCodeBits
     static constexpr int QW = F32 ? HD / 4 : HD / 8;                         // words of Q per lane
 
     uint32_t q[NB][QW];
@@ -515,13 +516,13 @@ struct PagedWave {
                     }
                 }
         } else {
-            if constexpr (F8) {                      // the values' powers of two go to the probabilities: exact
+            if constexpr (F8) {                      // the values' powers of two go to the probabilities, but for 2^kCodeBits, which the codes take: up to 2^8 times 2^127 overflows
                 const uint32_t s0 = lds_read<uint32_t>(at + 2 * kPart + 32 + 4 * g), s1 = lds_read<uint32_t>(at + 2 * kPart + 48 + 4 * g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float vs = exp2_of((int)(((j < 4 ? s0 : s1) >> (8 * (j & 3))) & 0xFFu));
+                    const int e = (int)(((j < 4 ? s0 : s1) >> (8 * (j & 3))) & 0xFFu) - (127 + kCodeBits);
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) p[b][j] = EDGE && p[b][j] == 0.f ? 0.f : p[b][j] * vs;
+                    for (int b = 0; b < NB; ++b) p[b][j] = __builtin_amdgcn_ldexpf(p[b][j], e);
                 }
             }
             // two bf16 terms of every probability
@@ -539,7 +540,8 @@ struct PagedWave {
                 if constexpr (F8) {
                     typedef int i32x2_t __attribute__((ext_vector_type(2)));
                     const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t *)(uintptr_t)(at + v_at[i]));
-                    v = u32x4_t{fp8_bf16x2<false>((uint32_t)x.x, 1.f), fp8_bf16x2<true>((uint32_t)x.x, 1.f), fp8_bf16x2<false>((uint32_t)x.y, 1.f), fp8_bf16x2<true>((uint32_t)x.y, 1.f)};
+                    constexpr float up = 1 << kCodeBits;
+                    v = u32x4_t{fp8_bf16x2<false>((uint32_t)x.x, up), fp8_bf16x2<true>((uint32_t)x.x, up), fp8_bf16x2<false>((uint32_t)x.y, up), fp8_bf16x2<true>((uint32_t)x.y, up)};
                 } else {
                     typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
                     using tr_t = __attribute__((address_space(3))) bf16x4_t;

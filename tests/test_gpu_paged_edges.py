@@ -237,3 +237,31 @@ def test_infinities_in_long_contexts(way):
     s = Setup([200, 1], [4800, 5000], 1, 64, torch.bfloat16, 64, seed=2)
     s.write_all()
     check_infinities(s, s.queries(4), [3, 2000])
+
+
+# ---- the ends of 8-bit exponents
+@pytest.mark.parametrize("heads", [(4, 2, 32), (8, 2, 64), (6, 1, 128)])
+@pytest.mark.parametrize("q_lens,kv_lens", [([1, 1], [300, 40]), ([6], [129]), ([200], [250])])
+@pytest.mark.parametrize("exponent", [1 + 127 - 80, 127, 127 + 90, 254])
+def test_powers_of_two_to_the_largest(way, heads, q_lens, kv_lens, exponent):
+    """V's codes are zeros and the smallest ones, its powers of two all the same: outputs are the same times that power, and zeros stay zeros."""
+    n_heads, n_kv, hd = heads
+    s = Setup(q_lens, kv_lens, n_kv, hd, F8, 16, seed=7)
+    v = torch.randint(-1, 2, (sum(kv_lens), n_kv, hd), generator=s.g, device=DEV).float() * 2.0 ** -9
+    v[:, :, 5] = 0.0
+    s.write_all(v=v)
+    s.cache.v_pages.copy_(torch.zeros_like(s.cache.v_pages))
+    s.cache.v_scales.fill_(exponent)
+    row = 0
+    for ids, kv in zip(s.ids, kv_lens):
+        for p in range(-(-kv // 16)):
+            n = min(16, kv - 16 * p)
+            s.cache.v_pages[ids[p], :, :n] = v[row:row + n].transpose(0, 1).to(F8)
+            row += n
+    s.v = [x.double() * 512 for x in v.split(kv_lens)]
+    q = s.queries(n_heads, 1.5)
+    got, lse = s.cache.attention(q, s.batch, want_lse=True)
+    back = torch.tensor(2.0, dtype=torch.float64, device=DEV) ** (9 + 127 - exponent)
+    assert bool((got[:, :, 5] == 0).all())
+    ref = exact_attention(s, q)
+    check_attention(s, q, (got.double() * back), lse, ref)
