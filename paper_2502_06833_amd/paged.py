@@ -58,14 +58,33 @@ def _code(t) -> int:
     return c
 
 
-def _rows(name, t, rows, heads, dim) -> Rows:
+def _rows(name, t, cache, rows, heads) -> Rows:
+    dim = cache.head_dim
     shape = t.shape
     if len(shape) != 3 or shape[0] != rows or shape[1] != heads or shape[2] != dim:
         raise ValueError(f"{name}: expected [{rows}, {heads}, {dim}], got {list(shape)}")
     s = t.stride()
-    if s[2] != 1 or not t.is_cuda:
-        raise ValueError(f"{name}: a tensor on the GPU whose last dimension is contiguous is needed")
+    if s[2] != 1 or t.get_device() != cache._device:
+        raise ValueError(f"{name}: a tensor on the cache's GPU whose last dimension is contiguous is needed")
     return Rows(t.data_ptr(), s[0], s[1])
+
+
+def _current_device():
+    """The current device's number (the accessor that returns it plainly, where this torch has it, looked up once)."""
+    global _current_device
+    import torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _current_device()
+
+
+def _stream(cache, batch):
+    """The current stream, for a call of the cache's device."""
+    if batch._device != cache._device:
+        raise ValueError(f"cache on GPU {cache._device}, batch on GPU {batch._device}: one is needed")
+    stream = _stream_ptr()
+    if _current_device() != cache._device:
+        raise ValueError(f"cache on GPU {cache._device}, but GPU {_current_device()} is the current one (torch.cuda.set_device, torch.cuda.device)")
+    return stream
 
 
 def _empty_like(q):
@@ -112,6 +131,7 @@ class PagedBatch:
             raise ValueError("page_table: its rows overlap (an expanded table?); .contiguous() gives every sequence its own")
         self.page_table, self.q_starts, self.kv_lens = page_table, q_starts, kv_lens
         self.rows = rows
+        self._device = page_table.get_device()
         self._desc = BatchDesc(n, rows, max_q, min_q, max_kv, stride, width, page_table.data_ptr(), q_starts.data_ptr(), kv_lens.data_ptr())
         self._ref = C.byref(self._desc)
         self._plans = {}
@@ -181,6 +201,7 @@ class PagedCache:
         ptr = [t.data_ptr() if t is not None else None for t in (k_pages, v_pages, k_scales, v_scales)]
         self._desc = CacheDesc(self._code, n, self.page_size, self.n_kv_heads, self.head_dim, *ptr)
         self._ref = C.byref(self._desc)
+        self._device = k_pages.get_device()
         self._key = (self._code, self.page_size, self.n_kv_heads, self.head_dim)
         self._attention = lib().ead_paged_attention
         self._scale = 1.0 / float(self.head_dim) ** 0.5
@@ -199,10 +220,11 @@ class PagedCache:
         code = _code(k)
         if v.dtype != k.dtype:
             raise ValueError(f"k and v of one type are needed, got {k.dtype} and {v.dtype}")
-        rk = _rows("k", k, batch.rows, self.n_kv_heads, self.head_dim)
-        rv = _rows("v", v, batch.rows, self.n_kv_heads, self.head_dim)
+        rk = _rows("k", k, self, batch.rows, self.n_kv_heads)
+        rv = _rows("v", v, self, batch.rows, self.n_kv_heads)
+        stream = _stream(self, batch)
         if batch.rows:
-            _check(lib().ead_paged_write(self._ref, batch._ref, code, C.byref(rk), C.byref(rv), _stream_ptr()))
+            _check(lib().ead_paged_write(self._ref, batch._ref, code, C.byref(rk), C.byref(rv), stream))
 
     def read(self, batch, dtype=None, out=None):
         """(k, v) [rows, n_kv_heads, head_dim] of the batch's rows, as `dtype` (bfloat16 if not said) or into `out`."""
@@ -213,10 +235,11 @@ class PagedCache:
         k, v = out
         if v.dtype != k.dtype:
             raise ValueError(f"out of one type is needed, got {k.dtype} and {v.dtype}")
-        rk = _rows("k", k, batch.rows, self.n_kv_heads, self.head_dim)
-        rv = _rows("v", v, batch.rows, self.n_kv_heads, self.head_dim)
+        rk = _rows("k", k, self, batch.rows, self.n_kv_heads)
+        rv = _rows("v", v, self, batch.rows, self.n_kv_heads)
+        stream = _stream(self, batch)
         if batch.rows:
-            _check(lib().ead_paged_read(self._ref, batch._ref, _code(k), C.byref(rk), C.byref(rv), _stream_ptr()))
+            _check(lib().ead_paged_read(self._ref, batch._ref, _code(k), C.byref(rk), C.byref(rv), stream))
         return out
 
     def attention(self, q, batch, window=0, sinks=0, scale=None, want_lse=False, out=None):
@@ -228,15 +251,15 @@ class PagedCache:
             raise ValueError(f"q: expected [rows, n_heads, {self.head_dim}], got {list(q.shape)}")
         if _code(q) != (F32 if self._code == F32 else BF16):
             raise ValueError(f"{q.dtype} queries over {self.k_pages.dtype} pages: float32 over float32, bfloat16 over the others")
-        rows, n_heads, dim = batch.rows, q.shape[1], self.head_dim
-        rq = _rows("q", q, rows, n_heads, dim)
+        rows, n_heads = batch.rows, q.shape[1]
+        rq = _rows("q", q, self, rows, n_heads)
         if out is None:
             out = _empty_like(q)
         elif out.dtype != q.dtype:
             raise ValueError(f"out: {q.dtype} is needed, got {out.dtype}")
-        ro = _rows("out", out, rows, n_heads, dim)
+        ro = _rows("out", out, self, rows, n_heads)
         lse = _empty_f32(q, rows, n_heads) if want_lse else None
-        stream = _stream_ptr()
+        stream = _stream(self, batch)
         p = batch._plan(self, n_heads, window, sinks, self._scale if scale is None else scale, stream)
         rc = self._attention(self._ref, batch._ref, p[0], C.byref(rq), C.byref(ro), lse.data_ptr() if want_lse else None, p[1], p[2], stream)
         if rc:

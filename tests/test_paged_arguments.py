@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2502_06833_amd as ead
+from paper_2502_06833_amd import paged
 
 
 class OnGpu:
@@ -10,6 +11,9 @@ class OnGpu:
 
     def __init__(self, t, device="cuda:0"):
         self.t, self.device, self.is_cuda = t, torch.device(device), True
+
+    def get_device(self):
+        return self.device.index
 
     def __getattr__(self, name):
         return getattr(self.t, name)
@@ -43,3 +47,34 @@ def test_strides_of_page_tables():
     assert d.table_width == 10 and d.table_stride >= 10
     d = batch_of(torch.arange(3, dtype=torch.int32).as_strided((1, 3), (0, 1)))._desc
     assert d.table_width == 3 and d.table_stride >= 3
+
+
+def cache_of(device="cuda:0", shape=(4, 2, 16, 64)):
+    return ead.PagedCache(*(OnGpu(torch.zeros(shape, dtype=torch.bfloat16), device) for _ in range(2)))
+
+
+def calls(cache, batch, k, q):
+    return [lambda: cache.write(k, k, batch), lambda: cache.read(batch, out=(k, k)), lambda: cache.attention(q, batch, out=q)]
+
+
+@pytest.mark.parametrize("where", [("cuda:1", "cuda:0", "cuda:0", 0), ("cuda:0", "cuda:1", "cuda:0", 0), ("cuda:0", "cuda:0", "cuda:1", 0),
+                                   ("cuda:0", "cuda:0", "cuda:0", 1), ("cuda:1", "cuda:1", "cuda:1", 0)])
+def test_tensors_of_different_devices_are_refused(monkeypatch, where):
+    """Cache, batch, rows and the current device, whose stream the kernels are launched on, have to be one."""
+    cache_on, batch_on, rows_on, current = where
+    monkeypatch.setattr(paged, "_current_device", lambda: current, raising=False)
+    monkeypatch.setattr(paged, "_stream_ptr", lambda: 0)
+    table = torch.zeros(2, 3, dtype=torch.int32)
+    k, q = OnGpu(torch.zeros(2, 2, 64, dtype=torch.bfloat16), rows_on), OnGpu(torch.zeros(2, 4, 64, dtype=torch.bfloat16), rows_on)
+    for call in calls(cache_of(cache_on), batch_of(table, batch_on), k, q):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_rows_on_the_host_are_refused(monkeypatch):
+    monkeypatch.setattr(paged, "_current_device", lambda: 0, raising=False)
+    monkeypatch.setattr(paged, "_stream_ptr", lambda: 0)
+    k, q = torch.zeros(2, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    for call in calls(cache_of(), batch_of(torch.zeros(2, 3, dtype=torch.int32)), k, q):
+        with pytest.raises(ValueError):
+            call()
