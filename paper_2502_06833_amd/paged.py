@@ -69,6 +69,14 @@ def _rows(name, t, cache, rows, heads) -> Rows:
     return Rows(t.data_ptr(), s[0], s[1])
 
 
+def _outputs(name, t, cache, rows, heads) -> Rows:
+    """The same for a tensor that is written: every vector needs a place of its own."""
+    r = _rows(name, t, cache, rows, heads)
+    if (rows > 1 and r.row_stride < cache.head_dim) or (heads > 1 and r.head_stride < cache.head_dim):
+        raise ValueError(f"{name}: vectors that overlap (strides {t.stride()}) cannot be written")
+    return r
+
+
 def _current_device():
     """The current device's number (the accessor that returns it plainly, where this torch has it, looked up once)."""
     global _current_device
@@ -235,8 +243,8 @@ class PagedCache:
         k, v = out
         if v.dtype != k.dtype:
             raise ValueError(f"out of one type is needed, got {k.dtype} and {v.dtype}")
-        rk = _rows("k", k, self, batch.rows, self.n_kv_heads)
-        rv = _rows("v", v, self, batch.rows, self.n_kv_heads)
+        rk = _outputs("k", k, self, batch.rows, self.n_kv_heads)
+        rv = _outputs("v", v, self, batch.rows, self.n_kv_heads)
         stream = _stream(self, batch)
         if batch.rows:
             _check(lib().ead_paged_read(self._ref, batch._ref, _code(k), C.byref(rk), C.byref(rv), stream))
@@ -257,7 +265,7 @@ class PagedCache:
             out = _empty_like(q)
         elif out.dtype != q.dtype:
             raise ValueError(f"out: {q.dtype} is needed, got {out.dtype}")
-        ro = _rows("out", out, self, rows, n_heads)
+        ro = _outputs("out", out, self, rows, n_heads)
         lse = _empty_f32(q, rows, n_heads) if want_lse else None
         stream = _stream(self, batch)
         p = batch._plan(self, n_heads, window, sinks, self._scale if scale is None else scale, stream)

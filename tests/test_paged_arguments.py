@@ -78,3 +78,22 @@ def test_rows_on_the_host_are_refused(monkeypatch):
     for call in calls(cache_of(), batch_of(torch.zeros(2, 3, dtype=torch.int32)), k, q):
         with pytest.raises(ValueError):
             call()
+
+
+def test_outputs_that_overlap_themselves_are_refused(monkeypatch):
+    """An expanded output has several rows or heads in one place; inputs may be expanded."""
+    monkeypatch.setattr(paged, "_current_device", lambda: 0)
+    monkeypatch.setattr(paged, "_stream_ptr", lambda: 0)
+    cache, batch = cache_of(), batch_of(torch.zeros(2, 3, dtype=torch.int32))
+    q, k = (OnGpu(torch.zeros(2, n, 64, dtype=torch.bfloat16)) for n in (4, 2))
+    flat = torch.zeros(1000, dtype=torch.bfloat16)
+    for strides in ((0, 64, 1), (256, 0, 1), (256, 32, 1), (32, 128, 1)):
+        with pytest.raises(ValueError):
+            cache.attention(q, batch, out=OnGpu(flat.as_strided((2, 4, 64), strides)))
+        with pytest.raises(ValueError):
+            cache.read(batch, out=(k, OnGpu(flat.as_strided((2, 2, 64), strides))))
+        with pytest.raises(ValueError):
+            cache.read(batch, out=(OnGpu(flat.as_strided((2, 2, 64), strides)), k))
+    # a dimension of 1 has no stride to speak of
+    one = ead.PagedCache(*(OnGpu(torch.zeros(4, 1, 16, 64, dtype=torch.bfloat16)) for _ in range(2)))
+    assert paged._outputs("out", OnGpu(flat.as_strided((2, 1, 64), (64, 0, 1))), one, 2, 1).row_stride == 64
