@@ -163,8 +163,8 @@ FewKernel few_kernel(const ead_paged_cache *c, int nb) {
     return k;
 }
 
-double g_small_work = kPagedSmallWork;                 // ead_test_paged's
-bool g_always_shares = false;
+thread_local double g_small_work = kPagedSmallWork;    // ead_test_paged's, for the calls of its thread
+thread_local bool g_always_shares = false;
 
 // The launches of a call: sequences with few rows (of a float32 cache: all), then those with many
 struct PagedCall {
@@ -284,7 +284,8 @@ ead_status ead_stream_capture(void *hip_stream, uint64_t *id) {
     return EAD_OK;
 }
 
-// For the tests alone, in no header: the work up to which one kernel takes a call alone (-1: as ever), and whether units are always cut into shares.
+// For the tests alone, in no header: the work up to which one kernel takes a call alone (-1: as ever), and whether units are always cut into shares, for
+// the calling thread.
 ead_status ead_test_paged(double small_work, int32_t always_shares) {
     g_small_work = small_work < 0 ? kPagedSmallWork : small_work;
     g_always_shares = always_shares != 0;

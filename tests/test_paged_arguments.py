@@ -1,4 +1,7 @@
 """What PagedBatch and PagedCache make of their tensors, without a GPU: stand-ins say that they lie on one."""
+import ctypes as C
+import threading
+
 import pytest
 import torch
 
@@ -97,3 +100,28 @@ def test_outputs_that_overlap_themselves_are_refused(monkeypatch):
     # a dimension of 1 has no stride to speak of
     one = ead.PagedCache(*(OnGpu(torch.zeros(4, 1, 16, 64, dtype=torch.bfloat16)) for _ in range(2)))
     assert paged._outputs("out", OnGpu(flat.as_strided((2, 1, 64), (64, 0, 1))), one, 2, 1).row_stride == 64
+
+
+def test_the_schedules_of_tests_are_their_threads_alone():
+    """ead_test_paged changes how the calling thread's calls are cut; another thread's workspaces stay what its launches need."""
+    L = ead.lib()
+    L.ead_test_paged.argtypes = [C.c_double, C.c_int32]
+    cache = paged.CacheDesc(1, 8, 16, 2, 64, 0x1000, 0x2000, None, None)
+    batch = paged.BatchDesc(1, 1, 1, 1, 100, 8, 8, 0x3000, 0x4000, 0x5000)
+    attn = paged.AttnDesc(4, 1, 0, 0, 0.125)
+
+    def need():
+        n = C.c_uint64(0)
+        assert L.ead_paged_workspace(C.byref(cache), C.byref(batch), C.byref(attn), C.byref(n)) == 0
+        return n.value
+
+    plain, other = need(), []
+    L.ead_test_paged(-1.0, 1)
+    try:
+        shares = need()
+        t = threading.Thread(target=lambda: other.append(need()))
+        t.start()
+        t.join()
+    finally:
+        L.ead_test_paged(-1.0, 0)
+    assert plain == 0 and shares > 0 and other == [plain] and need() == plain
