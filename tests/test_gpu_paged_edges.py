@@ -265,3 +265,28 @@ def test_powers_of_two_to_the_largest(way, heads, q_lens, kv_lens, exponent):
     assert bool((got[:, :, 5] == 0).all())
     ref = exact_attention(s, q)
     check_attention(s, q, (got.double() * back), lse, ref)
+
+
+# ---- pages behind a window
+def test_a_pair_in_a_pool_that_only_a_window_makes_do_with():
+    """The pair of paged_pair.py with 15 pages for three sequences of up to 140 positions (9 pages each): with a window the run fits, token for
+    token the one in a large pool, so no page went back that was still used; without one the pool runs out."""
+    import paged_pair
+    import synth_inputs as si
+    weights = [si.model_weights_torch(s, 0, "cuda") for s in (si.TINY_S, si.TINY_L)]
+    prompts = [si.prompt_np(0, f"pp{i}", n, si.TINY_S.vocab) for i, n in enumerate((5, 40, 23))]
+
+    def run(n_pages, window, sinks, tau):
+        models = [paged_pair.PagedModel(s, w, torch.float32, n_pages=n_pages, window=window, sinks=sinks) for s, w in zip((si.TINY_S, si.TINY_L), weights)]
+        out, _, _ = paged_pair.run(models, prompts, [0, 2, 9], 100, tau=tau, d_min=4, piece=8)
+        assert all(len(m.free) == n_pages for m in models)
+        return out
+
+    small = run(256, 20, 4, 1e30)
+    tau = sorted(x for o in small for x in o["Hbar"])[150]
+    wide, tight = run(256, 20, 4, tau), run(15, 20, 4, tau)
+    for a, b in zip(wide, tight):
+        assert a["tokens"] == b["tokens"] and a["model_id"] == b["model_id"] and a["H"] == b["H"]
+    assert len({m for o in wide for m in o["model_id"]}) == 2
+    with pytest.raises(RuntimeError, match="no free page"):
+        run(15, 0, 0, tau)
