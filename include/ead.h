@@ -332,11 +332,13 @@ ead_status ead_paged_read(const ead_paged_cache *cache, const ead_paged_batch *b
  * Scores, statistics and sums are float32; sums are divided by that of the exponentials at the end, and values within
  * some powers of two of the largest float may overflow in them.  8-bit vectors of V whose power of two is below 2^-90
  * lose bits (errors of up to 2^-100).  Over 16- and 8-bit pages probabilities enter their product as two bf16
- * terms (16 bits), as one in calls of many rows per KV head over more than 4096 keys except at the masks' edges.
+ * terms (16 bits).  one_term != 0 lets sequences of many rows per KV head (prompts) take one (8 bits) away from the
+ * masks' edges: a quarter less time over thousands of keys, an error of 0.0023 of the output's norm instead of 0.0017.
  * n_heads / n_kv_heads is an integer from 1 to 64; scale is positive. */
 typedef struct {
     int32_t n_heads, dtype, window, sinks;
     float scale;
+    int32_t one_term;
 } ead_paged_attn;
 /* Bytes of device memory an attention call needs (0 possible), 16-byte aligned.  The caller clears them once, before
  * the first call that gets them; every call leaves what the next one of the same cache layout, bounds of the batch

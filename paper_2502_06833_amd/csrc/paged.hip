@@ -168,7 +168,7 @@ thread_local bool g_always_shares = false;
 
 // The launches of a call: sequences with few rows (of a float32 cache: all), then those with many
 struct PagedCall {
-    bool few, many, two;
+    bool few, many;
     int few_rows;
     FewKernel kernel;
     PagedShares f;
@@ -196,7 +196,6 @@ PagedCall plan_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_
     }
     if (p.many) {
         p.m = paged_many(b->batch, c->n_kv_heads, group, rows, held, at->window, at->sinks, cus, c->head_dim);
-        p.two = paged_keys(128, 64, group, held, at->window, at->sinks) <= kPagedTwoTerms;
         p.m_bytes = paged_workspace(p.m.units, p.m.splits > 1 ? p.m.units * p.m.splits : 0, p.m.tile_rows, c->head_dim);
     }
     return p;
@@ -266,8 +265,8 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
         with_cache(cache, [&](auto ct, auto hd) {
             using CT = decltype(ct);
             if constexpr (sizeof(CT) != 4) {
-                if (p.two) hipLaunchKernelGGL((k_paged_chunk<CT, decltype(hd)::value, true>), grid, dim3(256), 0, st, c);
-                else hipLaunchKernelGGL((k_paged_chunk<CT, decltype(hd)::value, false>), grid, dim3(256), 0, st, c);
+                if (attn->one_term) hipLaunchKernelGGL((k_paged_chunk<CT, decltype(hd)::value, false>), grid, dim3(256), 0, st, c);
+                else hipLaunchKernelGGL((k_paged_chunk<CT, decltype(hd)::value, true>), grid, dim3(256), 0, st, c);
             }
         });
     }

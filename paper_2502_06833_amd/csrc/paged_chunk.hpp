@@ -17,10 +17,10 @@ constexpr int kChunkRows = 128;      // rows of a workgroup, 32 to a wave
 //   of 32: its statistics are its own up to one exchange of the wave's halves, and the scores of 16 keys, rounded to bf16, are the
 //   operand that O^T = V^T P^T wants if V's keys are taken in the same order.  V^T's operand comes from LDS by transposing reads.
 //
-//  Probabilities enter the second product as bf16.  One term of each is off by up to 2^-8 of it, which beside the rounding of the output
-//  makes the result's error against 64 bits 0.0023 of its norm instead of 0.0017; a second term (what the first leaves, rounded) takes that away for
-//  half as many products again.  Rows at a mask's edge, among them all that see few keys, always have both; the other tiles have both where no row of
-//  the launch sees more than kPagedTwoTerms keys (TWO): 4096 rows over 12289 .. 16384 keys of 32 heads take 1020 us with one term, 1400 with two.
+//  Probabilities enter the second product as bf16: in two terms (TWO), or in one away from the masks' edges where the caller asks for that.  One term of each is off
+//  by up to 2^-8 of it, which beside the rounding of the output makes the result's error against 64 bits 0.0022 to 0.0023 of its norm instead of 0.0017,
+//  over 600 keys as over 16000; a second term (what the first leaves, rounded) takes that away for half as many products again (2048 rows of
+//  32 heads over up to 4096, 9000 and 16000 bf16 keys: 129, 356 and 538 us with one term, 172, 461 and 708 with two; 8-bit keys 152, 395, 631 and 181, 492, 765).
 template <typename CT, int HD, bool TWO>
 __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttn c) {
     constexpr bool F8 = sizeof(CT) == 1;

@@ -4,7 +4,6 @@
 
 namespace ead {
 
-
 // Whether a write or a read moves more than stays in the second-level caches (32 MB) for who comes next
 inline bool paged_copy_streams(long rows, int n_kv, int head_dim, int bytes) { return 2.0 * rows * n_kv * head_dim * bytes > 64e6; }
 
@@ -13,9 +12,6 @@ constexpr int paged_max_blocks(int head_dim) { return head_dim == 128 ? 2 : 4; }
 
 // Rows per KV head (new tokens times query heads per KV head) of a sequence up to which k_paged_attn takes it
 constexpr int paged_few_rows(int head_dim) { return head_dim == 128 ? 32 : 64; }
-
-// Keys a row sees at most up to which k_paged_chunk takes two bf16 terms of every probability (its comment has both sides)
-constexpr int kPagedTwoTerms = 4096;
 
 // Ranges of keys of k_paged_chunk at most: their maxima and sums are joined in the LDS of a key tile
 constexpr int paged_many_splits(int head_dim) { return head_dim / 4; }

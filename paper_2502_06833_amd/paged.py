@@ -32,7 +32,8 @@ class Rows(C.Structure):
 
 
 class AttnDesc(C.Structure):
-    _fields_ = [("n_heads", C.c_int32), ("dtype", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("scale", C.c_float)]
+    _fields_ = [("n_heads", C.c_int32), ("dtype", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("scale", C.c_float),
+                ("one_term", C.c_int32)]
 
 
 def _check(rc):
@@ -170,14 +171,14 @@ class PagedBatch:
             self._of_capture = (n.value, {})
         return self._of_capture[1]
 
-    def _plan(self, cache, n_heads, window, sinks, scale, stream):
+    def _plan(self, cache, n_heads, window, sinks, scale, one_term, stream):
         """The attention arguments, and the workspace of this stream: cleared once, then every call leaves it ready for the next."""
         plans = self._captured_plans(stream) if _capturing() else self._plans
-        key = (stream, cache._key, n_heads, window, sinks, scale)
+        key = (stream, cache._key, n_heads, window, sinks, scale, one_term)
         p = plans.get(key)
         if p is None:
             import torch
-            d = AttnDesc(n_heads, F32 if cache._code == F32 else BF16, window, sinks, scale)
+            d = AttnDesc(n_heads, F32 if cache._code == F32 else BF16, window, sinks, scale, one_term)
             need = C.c_uint64(0)
             _check(lib().ead_paged_workspace(cache._ref, self._ref, C.byref(d), C.byref(need)))
             ws = torch.zeros((need.value + 3) // 4, dtype=torch.int32, device=self.kv_lens.device) if need.value else None
@@ -250,11 +251,13 @@ class PagedCache:
             _check(lib().ead_paged_read(self._ref, batch._ref, _code(k), C.byref(rk), C.byref(rv), stream))
         return out
 
-    def attention(self, q, batch, window=0, sinks=0, scale=None, want_lse=False, out=None):
+    def attention(self, q, batch, window=0, sinks=0, scale=None, want_lse=False, out=None, one_term=False):
         """softmax(scale q K^T) V of the batch's rows over their sequences, [rows, n_heads, head_dim] of q's type: float32
         over a float32 cache, bfloat16 over the others.  A row sees the positions up to its own; with window > 0 the last
         `window` of them and the first `sinks` of the sequence.  scale: 1 / sqrt(head_dim) if not said.  want_lse: also the
-        logarithm of the sum of exponentials, [rows, n_heads] float32.  Rows that see nothing get 0 and -inf."""
+        logarithm of the sum of exponentials, [rows, n_heads] float32.  Rows that see nothing get 0 and -inf.  one_term:
+        prompts' rows over 16- and 8-bit pages may take their probabilities with 8 bits instead of 16, for a quarter less time over
+        thousands of keys (error against 64 bits 0.0023 of the output's norm instead of 0.0017)."""
         if q.dim() != 3:
             raise ValueError(f"q: expected [rows, n_heads, {self.head_dim}], got {list(q.shape)}")
         if _code(q) != (F32 if self._code == F32 else BF16):
@@ -268,7 +271,7 @@ class PagedCache:
         ro = _outputs("out", out, self, rows, n_heads)
         lse = _empty_f32(q, rows, n_heads) if want_lse else None
         stream = _stream(self, batch)
-        p = batch._plan(self, n_heads, window, sinks, self._scale if scale is None else scale, stream)
+        p = batch._plan(self, n_heads, window, sinks, self._scale if scale is None else scale, one_term, stream)
         rc = self._attention(self._ref, batch._ref, p[0], C.byref(rq), C.byref(ro), lse.data_ptr() if want_lse else None, p[1], p[2], stream)
         if rc:
             _check(rc)

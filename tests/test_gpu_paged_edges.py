@@ -290,3 +290,65 @@ def test_a_pair_in_a_pool_that_only_a_window_makes_do_with():
     assert len({m for o in wide for m in o["model_id"]}) == 2
     with pytest.raises(RuntimeError, match="no free page"):
         run(15, 0, 0, tau)
+
+
+# ---- terms of probabilities
+def norm_error(got, out):
+    return float((got.double() - out).norm() / out.norm())
+
+
+# Rounding to bf16 is off by 2^-7 / sqrt(12) of the leading bit, 0.0016 of values spread over a binade, for the output's rounding alone; one bf16 term of
+# each probability adds as much again, independent of it: 0.0023.  In between, and above:
+TWO_TERMS, ONE_TERM = 0.0020, 0.0026
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, F8])
+@pytest.mark.parametrize("heads", [(8, 2, 64), (4, 1, 128), (4, 4, 32)])
+def test_rounding_of_probabilities(dtype, heads):
+    """Two terms for every row, whatever the other sequences' lengths or the bounds; one where the caller says so."""
+    n_heads, n_kv, hd = heads
+    lens = [700, 450, 300, 300, 260], [700, 2000, 4000, 9000, 5000]
+    s = Setup(*lens, n_kv, hd, dtype, 64, seed=1)
+    s.write_all()
+    q = s.queries(n_heads, 1.5)
+    generous = ead.PagedBatch(s.batch.page_table, s.batch.q_starts, s.batch.kv_lens, rows=sum(lens[0]), max_q=700, min_q=260, max_kv=10 ** 6)
+    for window, sinks in ((0, 0), (4500, 100), (2000, 100)):
+        out, z, _ = exact_attention(s, q, window, sinks)
+        for batch in (s.batch, generous):
+            for one_term in (False, True):
+                got, lse = s.cache.attention(q, batch, window=window, sinks=sinks, want_lse=True, one_term=one_term)
+                errors = [norm_error(a, b) for a, b in zip(got.split(lens[0]), out.split(lens[0]))]
+                assert max(errors) <= (ONE_TERM if one_term else TWO_TERMS), errors
+                assert float((lse.double() - z).abs().max()) <= 1e-5
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads", [(6, 2, 64), (8, 1, 128), (24, 1, 32)])
+@pytest.mark.parametrize("q_lens,kv_lens,window,sinks", [
+    ([130, 257], [130, 400], 0, 0), ([150, 1, 0], [600, 900, 5], 64, 33), ([200, 33], [333, 40], 129, 0), ([90], [2], 0, 0), ([700, 450], [5000, 4700], 0, 0),
+])
+def test_one_term(way, dtype, heads, q_lens, kv_lens, window, sinks):
+    """A term is off by at most 2^-8 of itself (8 significant bits), and so is the output's rounding: 1.05 * 2^-8 (|out| + sum_j p_j |v_j|) + 1e-5."""
+    n_heads, n_kv, hd = heads
+    s = Setup(q_lens, kv_lens, n_kv, hd, dtype, 64, seed=1)
+    s.write_all()
+    q = s.queries(n_heads, 1.5)
+    got, lse = s.cache.attention(q, s.batch, window=window, sinks=sinks, want_lse=True, one_term=True)
+    out, z, mass = exact_attention(s, q, window, sinks)
+    if dtype == torch.float32:                                # float32 pages take no terms
+        return check_attention(s, q, got, lse, (out, z, mass))
+    assert bool(((got.double() - out).abs() <= 1.05 * 2.0 ** -8 * (out.abs() + mass) + 1e-5).all())
+    assert torch.equal(torch.isinf(lse), torch.isinf(z))
+    f = torch.isfinite(z)
+    assert float((lse.double() - z)[f].abs().max() if f.any() else 0.0) <= 1e-5
+
+
+def test_one_term_of_infinities(way):
+    """An infinity that a row sees is its output with one term too."""
+    s = Setup([200], [700], 1, 128, torch.bfloat16, 16, seed=2)
+    s.write_all()
+    v = torch.cat(s.v).float()
+    v[97, :, 10], v[97, :, 11] = torch.inf, -torch.inf
+    s.write_all(k=torch.cat(s.k).float(), v=v)
+    got = s.cache.attention(s.queries(4), s.batch, one_term=True)
+    assert bool((got[:, :, 10] == torch.inf).all()) and bool((got[:, :, 11] == -torch.inf).all()) and bool(torch.isfinite(got[:, :, 12:]).all())
