@@ -334,7 +334,7 @@ ead_status ead_paged_read(const ead_paged_cache *cache, const ead_paged_batch *b
  * lose bits (errors of up to 2^-100).  Over 16- and 8-bit pages probabilities enter their product as two bf16
  * terms (16 bits).  one_term != 0 lets sequences of many rows per KV head (prompts) take one (8 bits) away from the
  * masks' edges: a quarter less time over thousands of keys, an error of 0.0023 of the output's norm instead of 0.0017.
- * n_heads / n_kv_heads is an integer from 1 to 64; scale is positive. */
+ * n_heads / n_kv_heads is an integer from 1 to 64; scale is positive, scale / ln 2 a float32. */
 typedef struct {
     int32_t n_heads, dtype, window, sinks;
     float scale;

@@ -25,6 +25,7 @@ ead_status refuse(ead_status st, const char *fmt, ...) {
 }
 #define PAGED_TRY(expr) do { ead_status s_ = (expr); if (s_ != EAD_OK) return s_; } while (0)
 
+constexpr float kLog2e = 1.4426950408889634f;
 int element_bytes(int dtype) { return dtype == EAD_F32 ? 4 : dtype == EAD_BF16 ? 2 : 1; }
 
 ead_status check_cache(const ead_paged_cache *c) {
@@ -134,7 +135,7 @@ ead_status check_attention(const ead_paged_cache *cache, const ead_paged_batch *
     if (at->dtype != (cache->dtype == EAD_F32 ? EAD_F32 : EAD_BF16))
         return refuse(EAD_ERR_INVALID_ARG, "queries are EAD_F32 over an EAD_F32 cache, EAD_BF16 over the others: got %d over %d", at->dtype, cache->dtype);
     if (at->window < 0 || at->sinks < 0) return refuse(EAD_ERR_INVALID_ARG, "window and sinks are 0 or more");
-    if (!(at->scale > 0.f) || !(at->scale < INFINITY)) return refuse(EAD_ERR_INVALID_ARG, "scale has to be positive and finite");
+    if (!(at->scale > 0.f) || !(at->scale * kLog2e < INFINITY)) return refuse(EAD_ERR_INVALID_ARG, "scale has to be positive, and scale / ln 2 finite");
     return EAD_OK;
 }
 
@@ -247,7 +248,7 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
     c.lse = lse;
     c.n_heads = attn->n_heads;
     c.group = attn->n_heads / cache->n_kv_heads;
-    c.c2 = attn->scale * 1.4426950408889634f;
+    c.c2 = attn->scale * kLog2e;
     c.window = attn->window;
     c.sinks = attn->sinks;
     c.few_rows = p.few_rows;

@@ -144,7 +144,7 @@ class PagedBatch:
         self._desc = BatchDesc(n, rows, max_q, min_q, max_kv, stride, width, page_table.data_ptr(), q_starts.data_ptr(), kv_lens.data_ptr())
         self._ref = C.byref(self._desc)
         self._plans = {}
-        self._of_capture = (0, {})
+        self._of_capture = (None, {})
 
     @classmethod
     def of(cls, page_table, q_lens, kv_lens):

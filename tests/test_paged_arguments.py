@@ -125,3 +125,13 @@ def test_the_schedules_of_tests_are_their_threads_alone():
     finally:
         L.ead_test_paged(-1.0, 0)
     assert plain == 0 and shares > 0 and other == [plain] and need() == plain
+
+
+def test_scales_whose_base_two_form_overflows_are_refused():
+    """Scores are kept in bits: scale * log2(e) has to be a float32 too."""
+    L = ead.lib()
+    cache = paged.CacheDesc(1, 8, 16, 2, 64, 0x1000, 0x2000, None, None)
+    batch = paged.BatchDesc(1, 1, 1, 1, 100, 8, 8, 0x3000, 0x4000, 0x5000)
+    for scale, status in ((2.3e38, 0), (2.4e38, 1), (3.4e38, 1)):
+        attn, n = paged.AttnDesc(4, 1, 0, 0, scale), C.c_uint64(0)
+        assert L.ead_paged_workspace(C.byref(cache), C.byref(batch), C.byref(attn), C.byref(n)) == status
