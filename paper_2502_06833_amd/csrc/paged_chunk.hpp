@@ -10,8 +10,8 @@ typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 constexpr int kChunkKeys = 64;       // keys of a tile
 constexpr int kChunkRows = 128;      // rows of a workgroup, 32 to a wave
 
-// Four waves take 32 rows each of a tile of 128, all of them every tile of 64 keys, which lands in LDS while the one before is
-// worked on (a bf16 cache: straight from memory, 1 KB a request; an 8-bit cache: its codes, which each
+// Four waves take 32 rows each of a tile of 128, all of them every tile of 64 keys, which is requested before the one before is worked on and lands in LDS
+// meanwhile, though as built a wave waits for it before its first product, whose operand Q the compiler loaded (a bf16 cache: straight from memory, 1 KB a request; an 8-bit cache: its codes, which each
 // wave turns into bf16 for the quarter of the keys that it asked for; in registers meanwhile, they cost 50 spilled ones).
 //   S^T = K Q^T with 32x32x16 products: lane (n, h) = (lane & 31, lane >> 5) gets row n's scores for keys 8 i + 4 h + 0..3, i = 0..3, of a block
 //   of 32: its statistics are its own up to one exchange of the wave's halves, and the scores of 16 keys, rounded to bf16, are the
