@@ -41,6 +41,13 @@ def _check(rc):
         raise EadError(rc, (lib().ead_last_error(None) or b"").decode())
 
 
+def _fits(**numbers):
+    """The descriptors hold 32 bits, to which ctypes cuts a number without a word."""
+    for name, n in numbers.items():
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise ValueError(f"{name}: {n} does not fit 32 bits")
+
+
 def _codes():
     import torch
     return {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: FP8}
@@ -138,6 +145,7 @@ class PagedBatch:
         stride = page_table.stride(0) if n > 1 else width         # a single row's stride says nothing
         if stride < width:
             raise ValueError("page_table: its rows overlap (an expanded table?); .contiguous() gives every sequence its own")
+        _fits(rows=rows, max_q=max_q, min_q=min_q, max_kv=max_kv, stride=stride)
         self.page_table, self.q_starts, self.kv_lens = page_table, q_starts, kv_lens
         self.rows = rows
         self._device = page_table.get_device()
@@ -178,6 +186,7 @@ class PagedBatch:
         p = plans.get(key)
         if p is None:
             import torch
+            _fits(window=window, sinks=sinks)
             d = AttnDesc(n_heads, F32 if cache._code == F32 else BF16, window, sinks, scale, one_term)
             need = C.c_uint64(0)
             _check(lib().ead_paged_workspace(cache._ref, self._ref, C.byref(d), C.byref(need)))
@@ -210,6 +219,7 @@ class PagedCache:
         ptr = [t.data_ptr() if t is not None else None for t in (k_pages, v_pages, k_scales, v_scales)]
         self._desc = CacheDesc(self._code, n, self.page_size, self.n_kv_heads, self.head_dim, *ptr)
         self._ref = C.byref(self._desc)
+        _fits(n_pages=n)
         self._device = k_pages.get_device()
         self._key = (self._code, self.page_size, self.n_kv_heads, self.head_dim)
         self._attention = lib().ead_paged_attention

@@ -135,3 +135,19 @@ def test_scales_whose_base_two_form_overflows_are_refused():
     for scale, status in ((2.3e38, 0), (2.4e38, 1), (3.4e38, 1)):
         attn, n = paged.AttnDesc(4, 1, 0, 0, scale), C.c_uint64(0)
         assert L.ead_paged_workspace(C.byref(cache), C.byref(batch), C.byref(attn), C.byref(n)) == status
+
+
+@pytest.mark.parametrize("bad", [2 ** 32 + 5, 2 ** 31, -2 ** 31 - 1])
+def test_numbers_that_do_not_fit_are_refused(monkeypatch, bad):
+    """The descriptors hold 32 bits, and ctypes would cut a larger number to them: 2^32 + 5 to 5."""
+    monkeypatch.setattr(paged, "_current_device", lambda: 0)
+    monkeypatch.setattr(paged, "_capturing", lambda: False)
+    monkeypatch.setattr(paged, "_stream_ptr", lambda: 0)
+    table = torch.zeros(2, 3, dtype=torch.int32)
+    for name in ("max_kv", "rows", "max_q", "min_q"):
+        with pytest.raises(ValueError):
+            batch_of(table, **{name: bad})
+    batch = batch_of(table)
+    for name in ("window", "sinks"):
+        with pytest.raises(ValueError):
+            batch._plan(cache_of(), 4, *({"window": (bad, 0), "sinks": (0, bad)}[name]), 0.125, False, 0)
