@@ -351,6 +351,89 @@ ead_status ead_paged_attention(const ead_paged_cache *cache, const ead_paged_bat
                                const ead_paged_attn *attn, const ead_rows *q, const ead_rows *out, float *lse,
                                void *workspace, uint64_t workspace_bytes, void *hip_stream);
 
+/* ---- the steps around it ------------------------------------------------------------ */
+
+/* Norms of queries and keys for each head, and the position rotation, in one pass.  A vector x of head_dim elements with a
+ * gain becomes x / sqrt(mean(x^2) + eps) * gain (without one it is left as it is); then its pairs i = 0 .. rotary_dim / 2 - 1 are turned
+ * by position * inv_freq[i] radians: (a, b) -> (a cos - b sin, b cos + a sin), the pairs being elements i and i + rotary_dim / 2
+ * ("rotate-half") or, interleaved != 0, 2 i and 2 i + 1.  Elements from rotary_dim on are not turned.  Sums, gains and products are
+ * float32, angles 64 bits; results are rounded once.  head_dim 32, 64 or 128; rotary_dim a multiple of 16 from 0 to head_dim. */
+typedef struct {
+    int32_t head_dim, rotary_dim, interleaved;
+    int32_t gain_per_head;          /* 0: q_gain, k_gain [head_dim] for all heads; otherwise [n_heads][head_dim] and [n_kv_heads][head_dim] */
+    float eps;
+    const double *inv_freq;         /* device [rotary_dim / 2] */
+    const float *q_gain, *k_gain;   /* device, null: queries (keys) are not normalised */
+} ead_rotary;
+/* q [rows][n_heads][head_dim] and k [rows][n_kv_heads][head_dim] of `dtype` (EAD_F32 or EAD_BF16) to q_out and k_out, which
+ * may be q and k themselves and otherwise do not overlap them; positions device [rows].  n_heads or n_kv_heads may be 0.
+ * Like the calls above, all of these are asynchronous on `hip_stream`, allocate nothing and can be captured in a graph. */
+ead_status ead_rotate(const ead_rotary *rotary, int32_t dtype, int32_t rows, int32_t n_heads, int32_t n_kv_heads,
+                      const int32_t *positions, const ead_rows *q, const ead_rows *k, const ead_rows *q_out,
+                      const ead_rows *k_out, void *hip_stream);
+/* The same on the way to a cache: the batch's queries to q_out, its keys (normalised and turned) and its values (as they are) to
+ * their places in the pages, rounded once.  positions device [rows], or null: the batch's own (kv_lens[b] - n + i), which differ
+ * from a text's once positions have been evicted.  Places are the batch's either way.  Rows of no sequence are not touched. */
+ead_status ead_paged_append(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_rotary *rotary, int32_t dtype,
+                            int32_t n_heads, const int32_t *positions, const ead_rows *q, const ead_rows *k, const ead_rows *v,
+                            const ead_rows *q_out, void *hip_stream);
+
+/* What the rows' attention pays to every cached position, per KV head, in float32 pages of their own:
+ *   weights [n_pages][n_kv_heads][page_size]:  w_j = (w_j before, 0 at the rows' own positions) + sum over the rows that see j
+ *                                              and the query heads of the group of exp(scale q.k_j - lse)
+ * with the arguments and the lse of ead_paged_attention for the same rows (lse [rows][n_heads]; a row whose lse is -infinity pays
+ * nothing).  New positions start from nothing, so pages need no clearing where every step's rows are weighed.  Sums are
+ * float32, in an order that the call's sizes fix (no atomics).  A page belongs to one sequence of the batch: what two sequences
+ * of a call pay to a page they share is not added up right.  attn->one_term is not looked at.  Workspaces as those of
+ * ead_paged_attention, but nothing has to clear them. */
+ead_status ead_paged_weigh_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_attn *attn,
+                                     uint64_t *bytes);
+ead_status ead_paged_weigh(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_attn *attn,
+                           const ead_rows *q, const float *lse, float *weights, void *workspace, uint64_t workspace_bytes,
+                           void *hip_stream);
+
+/* Cuts every sequence that holds more than `keep` positions to that many, each KV head by its own scores (float32 pages as
+ * `weights` above, for instance those): the first `sinks` and the last `recent` positions stay, and of the others the keep - sinks - recent
+ * with the largest scores (of equal ones the lower positions; -0 is 0, NaN is below everything).  Those of them that lie below
+ * keep - recent stay where they are, the others go, in their order, to the places there that became free; the last positions follow at
+ * keep - recent, in their order.  K, V, their scales and `weights` (null: none; may be the scores) move; kept[b][h][i] is the position that now lies at
+ * i, -1 from the sequence's length on.  kv_lens is not changed, since other layers' caches still need it: afterwards the
+ * sequence holds min(kv_len, keep) positions.  q_starts, rows and max_q are not looked at.  Holes have the score 0; what is moved
+ * from one is zeros, what is moved to one is lost.  The sequences' pages are theirs alone. */
+typedef struct { int32_t keep, sinks, recent; } ead_paged_eviction;
+/* Bytes of device memory the call needs, 16-byte aligned; nothing has to clear them, and no two calls at once share them. */
+ead_status ead_paged_evict_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_eviction *eviction,
+                                     uint64_t *bytes);
+ead_status ead_paged_evict(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_eviction *eviction,
+                           const float *scores, float *weights, int32_t *kept, void *workspace, uint64_t workspace_bytes,
+                           void *hip_stream);
+
+/* ---- log probabilities of given tokens, beside the entropy ---------------------------- */
+
+/* From logits [rows][vocab] (`dtype` EAD_F32 or EAD_BF16, row_stride elements apart, at any alignment), in one pass:
+ *   logprob [rows]   ln softmax(l)[token] of tokens[row], and rank [rows], 1 + the number of larger logits; both 0 for a token outside
+ *                    0 .. vocab-1 (-1: none)
+ *   H [rows]         the entropy, in `unit`
+ *   top_tokens, top_logprobs [rows][top]   the most likely tokens, equal logits in the tokens' order (so [0] is ead_entropy_argmax's
+ *                    token), and their ln softmax
+ * All outputs are device pointers; tokens, logprob, rank and H may be null; top is 0 .. 32.  A logit of -infinity has probability 0.  A row with a NaN or a
+ * +infinity, or with nothing above -infinity, has NaN for all its numbers; its tokens are ordered with NaN as -infinity.
+ * rows up to 2^22, vocab up to 2^24. */
+typedef struct {
+    const void *logits;
+    int32_t dtype, rows, vocab;
+    int64_t row_stride;
+    const int32_t *tokens;
+    int32_t top, unit;
+    float *logprob, *H;
+    int32_t *rank, *top_tokens;
+    float *top_logprobs;
+} ead_logprob_call;
+/* Bytes of device memory a call of that rows, vocab and top needs (0 possible), 16-byte aligned.  The caller clears them once;
+ * every call leaves what the next one expects, of whatever shape.  A workspace serves one stream at a time, or one graph. */
+ead_status ead_logprobs_workspace(const ead_logprob_call *call, uint64_t *bytes);
+ead_status ead_logprobs(const ead_logprob_call *call, void *workspace, uint64_t workspace_bytes, void *hip_stream);
+
 /* ---- bookkeeping ----------------------------------------------------------------- */
 ead_status ead_get_stats(ead_handle *h, ead_stats *out);
 ead_status ead_reset_stats(ead_handle *h);

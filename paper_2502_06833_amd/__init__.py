@@ -7,3 +7,5 @@ There is no CPU fallback: loading fails loudly if the library has not been built
 from .binding import (EAD, BITS, NATS, SMALL, LARGE, EadError, Gate, entropy_argmax, lib,  # noqa: F401
                       exported_symbols)
 from .paged import PagedBatch, PagedCache  # noqa: F401
+from .rotary import Rotary  # noqa: F401
+from .scoring import LogProbs, logprobs  # noqa: F401

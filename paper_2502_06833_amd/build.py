@@ -7,8 +7,9 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libead.so")
-SOURCES = ["ead.hip", "paged.hip"]
-HEADERS = ["common.hpp", "linear.hpp", "attention.hpp", "entropy.hpp", "rules.hpp", "state.hpp", "fused.hpp", "stream_list.hpp", "stream.hpp", "turn.hpp", "paged.hpp", "paged_chunk.hpp", "paged_rules.hpp"]
+SOURCES = ["ead.hip", "paged.hip", "paged_steps.hip", "logprobs.hip"]
+HEADERS = ["common.hpp", "linear.hpp", "attention.hpp", "entropy.hpp", "rules.hpp", "state.hpp", "fused.hpp", "stream_list.hpp", "stream.hpp", "turn.hpp", "paged.hpp", "paged_chunk.hpp", "paged_rules.hpp", "paged_host.hpp",
+           "rotate.hpp", "weigh.hpp", "evict.hpp", "logprobs.hpp"]
 
 
 def _newest_source() -> float:

@@ -105,4 +105,39 @@ inline PagedPlan paged_many(int batch, int n_kv, int group, long rows, int max_k
     return paged_cut(128, 64, rows, batch, n_kv, group, max_kv, window, sinks, 2l * cus, 4, paged_many_splits(head_dim));
 }
 
+// Groups of lanes that share a row of queries, keys (and values) whose heads are normalised and turned: a head to each while the rows do not fill the device, then fewer,
+// which compute a row's sines and cosines less often.
+inline int rotate_groups(long rows, int heads, int head_dim) {
+    const long lanes = rows * heads * (head_dim / 16), each = std::max(1l, lanes / (256l * 2048));
+    return (int)std::max(1l, (heads + each - 1) / each);
+}
+
+// ---- eviction ----
+constexpr int kEvictCached = 12288;        // scores of a sequence and head that a workgroup keeps in LDS
+inline unsigned long long evict_moves_at(unsigned long long units) { return (units * 4 + 15) / 16 * 16; }
+struct EvictPlan {
+    int threads;                           // of a workgroup that chooses
+    int columns;                           // pieces of a vector that workgroups of their own move
+};
+inline EvictPlan evict_plan(int batch, int n_kv, int held, int vec_bytes, int cus) {
+    EvictPlan p;
+    p.threads = held > 4096 ? 1024 : 256;
+    p.columns = 1;
+    while (vec_bytes / p.columns > 64 && 2l * batch * n_kv * p.columns < 2l * cus) p.columns *= 2;
+    return p;
+}
+
+// ---- log probabilities ----
+// Workgroups of four waves that a row of logits goes to, and sets of `set` vectors to each (a row that does not start on a 16-byte boundary has up to one vector more)
+struct LogprobPlan { int parts, part_sets; };
+constexpr int kLogprobTickets = 1024;      // rows that may be cut: with more there is a workgroup for every compute unit anyway
+inline LogprobPlan logprob_plan(long rows, int vocab, int set, int cus) {
+    const long sets = ((vocab + 14) / 8 + set - 1) / set, most = (sets + 3) / 4;
+    const long want = rows > kLogprobTickets ? 1 : std::max(1l, std::min(most, 4l * cus / std::max(1l, rows)));
+    LogprobPlan p;
+    p.part_sets = (int)((sets + 4 * want - 1) / (4 * want)) * 4;
+    p.parts = (int)((sets + p.part_sets - 1) / p.part_sets);
+    return p;
+}
+
 }  // namespace ead

@@ -5,6 +5,13 @@
     cache.write(k, v, batch)                        # the new tokens' keys and values
     out = cache.attention(q, batch, window=4096, sinks=4)
 
+and the steps around it (`Rotary` is in rotary.py):
+
+    q = cache.append(q, k, v, batch, rotary)        # queries and keys normalised and rotated, keys and values written
+    out, lse = cache.attention(q, batch, want_lse=True)
+    cache.weigh(q, lse, batch, weights)             # what every position is paid, added up in weights = cache.new_weights()
+    kept = cache.evict(batch, weights, 2048, sinks=4, recent=256)    # afterwards sequences hold kv_lens.clamp(max=2048) positions
+
 `kv_lens` count the new tokens: sequence b's rows are the last `q_lens[b]` of its `kv_lens[b]` positions.
 """
 from __future__ import annotations
@@ -34,6 +41,10 @@ class Rows(C.Structure):
 class AttnDesc(C.Structure):
     _fields_ = [("n_heads", C.c_int32), ("dtype", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("scale", C.c_float),
                 ("one_term", C.c_int32)]
+
+
+class EvictionDesc(C.Structure):
+    _fields_ = [("keep", C.c_int32), ("sinks", C.c_int32), ("recent", C.c_int32)]
 
 
 def _check(rc):
@@ -194,6 +205,30 @@ class PagedBatch:
             p = plans[key] = (C.byref(d), ws.data_ptr() if need.value else None, need.value, d, ws)
         return p
 
+    def _sized(self, what, cache, args, describe):
+        """A call's descriptor and the bytes of the workspace it wants, which nothing has to clear."""
+        key = (what, cache._key, args)
+        p = self._plans.get(key)
+        if p is None:
+            d = describe(*args)
+            need = C.c_uint64(0)
+            _check(getattr(lib(), what)(cache._ref, self._ref, C.byref(d), C.byref(need)))
+            p = self._plans[key] = (C.byref(d), need.value, d)
+        return p
+
+
+def _scratch(like, need):
+    """Device memory for one call on the current stream (or in the graph that is being captured)."""
+    import torch
+    return like.new_empty((need + 3) // 4, dtype=torch.int32) if need else None
+
+
+def _positions(t, rows, device):
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != rows or (rows > 1 and t.stride(0) != 1) or t.get_device() != device:
+        raise ValueError(f"positions: int32 [{rows}], contiguous and on the same GPU, is needed")
+    return t.data_ptr()
+
 
 class PagedCache:
     """The cache of one attention layer: k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim] in float32, bfloat16 or
@@ -286,3 +321,87 @@ class PagedCache:
         if rc:
             _check(rc)
         return (out, lse) if want_lse else out
+
+    def append(self, q, k, v, batch, rotary, positions=None, out=None):
+        """The batch's queries [rows, n_heads, head_dim] normalised and turned (into `out`, or a new tensor; `out` may be q), its keys
+        likewise and its values as they are written to their places, all in one pass.  q, k, v: float32 or bfloat16, any row and head strides.
+        rotary: a Rotary.  positions: int32 [rows]; the batch's own if not said, which are a text's as long as nothing has been evicted."""
+        if q.dim() != 3:
+            raise ValueError(f"q: expected [rows, n_heads, {self.head_dim}], got {list(q.shape)}")
+        code = _code(q)
+        if code == FP8 or k.dtype != q.dtype or v.dtype != q.dtype:
+            raise ValueError(f"q, k and v of one type, float32 or bfloat16, are needed, got {q.dtype}, {k.dtype} and {v.dtype}")
+        rows, n_heads = batch.rows, q.shape[1]
+        rotary._fits(self.head_dim, self._device, n_heads, self.n_kv_heads)
+        rq = _rows("q", q, self, rows, n_heads)
+        rk = _rows("k", k, self, rows, self.n_kv_heads)
+        rv = _rows("v", v, self, rows, self.n_kv_heads)
+        if out is None:
+            out = _empty_like(q)
+        elif out.dtype != q.dtype:
+            raise ValueError(f"out: {q.dtype} is needed, got {out.dtype}")
+        ro = _outputs("out", out, self, rows, n_heads)
+        at = None if positions is None else _positions(positions, rows, self._device)
+        stream = _stream(self, batch)
+        if rows:
+            _check(lib().ead_paged_append(self._ref, batch._ref, rotary._ref, code, n_heads, at, C.byref(rq), C.byref(rk), C.byref(rv), C.byref(ro), stream))
+        return out
+
+    def new_weights(self):
+        """Float32 pages for `weigh`, [n_pages, n_kv_heads, page_size], all zero."""
+        import torch
+        return torch.zeros(self.k_pages.shape[:3], dtype=torch.float32, device=self.k_pages.device)
+
+    def _pool(self, name, t):
+        import torch
+        if t.dtype != torch.float32 or t.shape != self.k_pages.shape[:3] or not t.is_contiguous() or t.get_device() != self._device:
+            raise ValueError(f"{name}: contiguous float32 {list(self.k_pages.shape[:3])} on the cache's GPU is needed")
+        return t.data_ptr()
+
+    def weigh(self, q, lse, batch, weights, window=0, sinks=0, scale=None):
+        """Adds to `weights` (float32 [n_pages, n_kv_heads, page_size], see new_weights) what the rows' attention pays to every position
+        they see, exp(scale q k - lse) over the rows and the query heads of a group; the rows' own positions start from nothing.  q, window, sinks and
+        scale as for `attention` of the same rows, lse as it returned it.  A page belongs to one sequence of the batch."""
+        if q.dim() != 3:
+            raise ValueError(f"q: expected [rows, n_heads, {self.head_dim}], got {list(q.shape)}")
+        if _code(q) != (F32 if self._code == F32 else BF16):
+            raise ValueError(f"{q.dtype} queries over {self.k_pages.dtype} pages: float32 over float32, bfloat16 over the others")
+        import torch
+        rows, n_heads = batch.rows, q.shape[1]
+        rq = _rows("q", q, self, rows, n_heads)
+        if lse.dtype != torch.float32 or lse.shape != (rows, n_heads) or not lse.is_contiguous() or lse.get_device() != self._device:
+            raise ValueError(f"lse: contiguous float32 [{rows}, {n_heads}] on the cache's GPU is needed")
+        to = self._pool("weights", weights)
+        stream = _stream(self, batch)
+        _fits(window=window, sinks=sinks)
+        args = (n_heads, F32 if self._code == F32 else BF16, window, sinks, self._scale if scale is None else scale, 0)
+        d, need, _ = batch._sized("ead_paged_weigh_workspace", self, args, AttnDesc)
+        ws = _scratch(lse, need)
+        _check(lib().ead_paged_weigh(self._ref, batch._ref, d, C.byref(rq), lse.data_ptr(), to, ws.data_ptr() if need else None, need, stream))
+        return weights
+
+    def evict(self, batch, scores, keep, sinks=0, recent=0, weights=None, kept=None):
+        """Cuts every sequence of more than `keep` positions to that many, each KV head for itself: the first `sinks` and the last `recent`
+        stay, and of the others those with the largest `scores` (float32 pages as those of `weigh`; of equal ones the lower positions).  The places
+        that became free are filled from behind and the last positions follow, so the first `sinks` and the last `recent` keep
+        their order.  `weights`: pages that move with the positions, `scores` if not said.  Returns int32 [sequences, n_kv_heads, keep]: which
+        position lies where now (-1 past a sequence's end).  batch.kv_lens stays as it is, for the other layers; then it is
+        kv_lens.clamp(max=keep)."""
+        import torch
+        _fits(keep=keep, sinks=sinks, recent=recent)
+        if keep < 1 or sinks < 0 or recent < 0 or sinks + recent > keep:
+            raise ValueError(f"keep {keep}, sinks {sinks}, recent {recent}: 1 or more, 0 or more, and sinks + recent <= keep are needed")
+        n = batch._desc.batch
+        of = self._pool("scores", scores)
+        to = of if weights is None else self._pool("weights", weights)
+        if kept is None:
+            kept = scores.new_empty((n, self.n_kv_heads, keep), dtype=torch.int32)
+        elif kept.dtype != torch.int32 or kept.shape != (n, self.n_kv_heads, keep) or not kept.is_contiguous() or kept.get_device() != self._device:
+            raise ValueError(f"kept: contiguous int32 {[n, self.n_kv_heads, keep]} on the cache's GPU is needed")
+        stream = _stream(self, batch)
+        if n == 0:
+            return kept
+        d, need, _ = batch._sized("ead_paged_evict_workspace", self, (keep, sinks, recent), EvictionDesc)
+        ws = _scratch(scores, need)
+        _check(lib().ead_paged_evict(self._ref, batch._ref, d, of, to, kept.data_ptr(), ws.data_ptr(), need, stream))
+        return kept

@@ -1,0 +1,81 @@
+"""Log probabilities of given tokens, entropies and the most likely tokens from logits (`ead_logprobs` of include/ead.h)."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import NamedTuple
+
+from .binding import BF16, F32, NATS, _stream_ptr, lib
+from . import paged
+from .paged import _check
+
+
+class CallDesc(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32), ("row_stride", C.c_int64), ("tokens", C.c_void_p),
+                ("top", C.c_int32), ("unit", C.c_int32), ("logprob", C.c_void_p), ("H", C.c_void_p), ("rank", C.c_void_p), ("top_tokens", C.c_void_p),
+                ("top_logprobs", C.c_void_p)]
+
+
+class LogProbs(NamedTuple):
+    H: object                   # [rows] float32: entropies
+    logprob: object = None      # [rows] float32: of the given tokens (0 where there is none)
+    rank: object = None         # [rows] int32: 1 + the number of larger logits (0 where there is no token)
+    top_tokens: object = None   # [rows, top] int32: the most likely tokens, equal ones in their order
+    top_logprobs: object = None  # [rows, top] float32
+
+
+class _Workspaces:
+    """One for each stream, cleared when it is made; calls leave it ready for the next.  A capture's calls have one for each of its streams, in the graph's memory and
+    cleared by a node of the graph."""
+
+    def __init__(self):
+        self._eager, self._captured = {}, (None, {})
+
+    def get(self, need, device, stream):
+        import torch
+        of, key = self._eager, (device.index, stream)
+        if paged._capturing():
+            n = C.c_uint64(0)
+            _check(lib().ead_stream_capture(C.c_void_p(stream), C.byref(n)))
+            if self._captured[0] != (device.index, n.value):
+                self._captured = ((device.index, n.value), {})
+            of = self._captured[1]
+        ws = of.get(key)
+        if ws is None or ws.numel() * 4 < need:
+            ws = of[key] = torch.zeros((need + 3) // 4, dtype=torch.int32, device=device)
+        return ws.data_ptr()
+
+
+_workspaces = _Workspaces()
+_dtypes = None
+
+
+def logprobs(logits, tokens=None, top=0, unit=NATS):
+    """logits [rows, vocab], bfloat16 or float32, any row stride; tokens: int32 [rows] (outside 0 .. vocab-1: none); top: alternatives, 0 .. 32.
+    Log probabilities are natural logarithms, entropies in `unit`.  Rows without a distribution (a NaN, +inf, nothing above -inf) have NaN."""
+    import torch
+    global _dtypes
+    if _dtypes is None:
+        _dtypes = {torch.float32: F32, torch.bfloat16: BF16}
+    code = _dtypes.get(logits.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {logits.dtype}")
+    if not logits.is_cuda or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1) or (logits.stride(0) < 0):
+        raise ValueError("logits: [rows, vocab] on the GPU whose rows are contiguous are needed")
+    rows, vocab = logits.shape
+    if vocab < 1 or top < 0 or top > min(32, vocab):
+        raise ValueError(f"top {top} is not in 0 .. {min(32, vocab)} (vocab {vocab})")
+    device = logits.get_device()
+    if tokens is not None and (tokens.dtype != torch.int32 or tokens.shape != (rows,) or (rows > 1 and tokens.stride(0) != 1) or tokens.get_device() != device):
+        raise ValueError(f"tokens: int32 [{rows}], contiguous and on the logits' GPU, is needed")
+    if paged._current_device() != device:
+        raise ValueError(f"logits on GPU {device}, but GPU {paged._current_device()} is the current one (torch.cuda.set_device, torch.cuda.device)")
+    f32, i32 = torch.float32, torch.int32
+    H = logits.new_empty(rows, dtype=f32)
+    lp, rank = (logits.new_empty(rows, dtype=f32), logits.new_empty(rows, dtype=i32)) if tokens is not None else (None, None)
+    tt, tl = (logits.new_empty((rows, top), dtype=i32), logits.new_empty((rows, top), dtype=f32)) if top else (None, None)
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    d = CallDesc(logits.data_ptr(), code, rows, vocab, logits.stride(0) if rows > 1 else vocab, ptr(tokens), top, unit, ptr(lp), H.data_ptr(), ptr(rank), ptr(tt), ptr(tl))
+    ref, need, stream = C.byref(d), C.c_uint64(0), _stream_ptr()
+    _check(lib().ead_logprobs_workspace(ref, C.byref(need)))
+    _check(lib().ead_logprobs(ref, _workspaces.get(need.value, logits.device, stream) if need.value else None, need.value, stream))
+    return LogProbs(H, lp, rank, tt, tl)
