@@ -54,6 +54,27 @@ ead_status check_weigh(const ead_paged_cache *cache, const ead_paged_batch *batc
 
 int held_of(const ead_paged_cache *c, const ead_paged_batch *b) { return (int)std::min((long)b->max_kv, (long)b->table_width * c->page_size); }
 
+// How a call of ead_paged_weigh is cut: the workspace is the same whatever the queries' alignment lets it do
+struct WeighCall {
+    bool few;
+    int blocks, tiles;
+    WeighPlan m;
+    uint64_t bytes;
+};
+WeighCall weigh_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead_paged_attn *at) {
+    const long rows = (long)b->max_q * (at->n_heads / c->n_kv_heads);
+    const int held = std::max(1, held_of(c, b));
+    WeighCall w{};
+    w.few = rows <= weigh_few_rows(c->dtype == EAD_F32, c->head_dim);
+    w.blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    w.tiles = weigh_tiles((long)b->batch * c->n_kv_heads, held, kWeighTiles, compute_units());
+    if (!w.few && c->dtype != EAD_F32) {
+        w.m = weigh_many(b->batch, c->n_kv_heads, rows, held, compute_units());
+        if (w.m.splits > 1) w.bytes = (uint64_t)w.m.splits * b->batch * c->n_kv_heads * w.m.part_keys * 4;
+    }
+    return w;
+}
+
 }  // namespace
 
 extern "C" {
@@ -116,7 +137,9 @@ ead_status ead_paged_append(const ead_paged_cache *cache, const ead_paged_batch 
 ead_status ead_paged_weigh_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_attn *attn, uint64_t *bytes) {
     if (!bytes) return refuse(EAD_ERR_INVALID_ARG, "bytes is null");
     *bytes = 0;
-    return check_weigh(cache, batch, attn);
+    PAGED_TRY(check_weigh(cache, batch, attn));
+    *bytes = weigh_of(cache, batch, attn).bytes;
+    return EAD_OK;
 }
 
 ead_status ead_paged_weigh(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_attn *attn, const ead_rows *q, const float *lse,
@@ -127,15 +150,40 @@ ead_status ead_paged_weigh(const ead_paged_cache *cache, const ead_paged_batch *
     if (((uintptr_t)lse | (uintptr_t)weights) & 3) return refuse(EAD_ERR_INVALID_ARG, "lse or weights is not aligned to its elements");
     PagedWeigh c{};
     PAGED_TRY(rows_of(q, attn->dtype, "q", &c.q));
+    const WeighCall w = weigh_of(cache, batch, attn);
+    if (w.bytes && (!workspace || workspace_bytes < w.bytes || ((uintptr_t)workspace & 15)))
+        return refuse(EAD_ERR_INVALID_ARG, "workspace: %llu bytes, 16-byte aligned, are needed", (unsigned long long)w.bytes);
     c.a = args_of(cache, batch);
     c.lse = lse; c.weights = weights;
     c.n_heads = attn->n_heads; c.group = attn->n_heads / cache->n_kv_heads;
     c.c2 = attn->scale * kLog2e;
     c.window = attn->window; c.sinks = attn->sinks;
-    const dim3 grid((unsigned)std::max(1, (held_of(cache, batch) + 63) / 64), (unsigned)cache->n_kv_heads, (unsigned)batch->batch);
-    with_cache(cache, [&](auto ct, auto hd) {
-        hipLaunchKernelGGL((k_weigh<decltype(ct), decltype(hd)::value>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
-    });
+    const int held = std::max(1, held_of(cache, batch));
+    const hipStream_t st = (hipStream_t)hip_stream;
+    if (w.few) {
+        c.tiles = w.tiles;
+        const dim3 grid((unsigned)((held + 128l * w.tiles - 1) / (128l * w.tiles) * cache->n_kv_heads), (unsigned)batch->batch);
+        with_cache(cache, [&](auto ct, auto hd) {
+            using CT = decltype(ct);
+            constexpr int HD = decltype(hd)::value;
+            if (w.blocks == 1) hipLaunchKernelGGL((k_weigh_few<CT, HD, 1>), grid, dim3(256), 0, st, c);
+            else if (w.blocks == 2) hipLaunchKernelGGL((k_weigh_few<CT, HD, 2>), grid, dim3(256), 0, st, c);
+            else if constexpr (weigh_few_rows(sizeof(CT) == 4, HD) == 64) hipLaunchKernelGGL((k_weigh_few<CT, HD, 4>), grid, dim3(256), 0, st, c);
+        });
+    } else if (cache->dtype != EAD_F32 && c.q.vec) {
+        c.splits = w.m.splits; c.part_keys = w.m.part_keys;
+        c.part = (float *)workspace;
+        const dim3 grid((unsigned)((long)cache->n_kv_heads * w.m.splits * (w.m.part_keys / 256)), (unsigned)batch->batch);
+        with_cache(cache, [&](auto ct, auto hd) {
+            using CT = decltype(ct);
+            if constexpr (sizeof(CT) != 4) hipLaunchKernelGGL((k_weigh_many<CT, decltype(hd)::value>), grid, dim3(256), 0, st, c);
+        });
+        if (w.m.splits > 1)
+            hipLaunchKernelGGL(k_weigh_join, dim3((unsigned)(w.m.part_keys / 256), (unsigned)cache->n_kv_heads, (unsigned)batch->batch), dim3(256), 0, st, c);
+    } else {
+        const dim3 grid((unsigned)((held + 63) / 64), (unsigned)cache->n_kv_heads, (unsigned)batch->batch);
+        with_cache(cache, [&](auto ct, auto hd) { hipLaunchKernelGGL((k_weigh<decltype(ct), decltype(hd)::value>), grid, dim3(256), 0, st, c); });
+    }
     return launched("ead_paged_weigh");
 }
 

@@ -12,6 +12,9 @@ struct PagedWeigh {
     int n_heads, group;             // group: query heads per KV head
     float c2;                       // scale * log2(e)
     int window, sinks;
+    int tiles;                      // k_weigh_few: tiles of 32 keys to a wave
+    int splits, part_keys;          // k_weigh_many: ranges of rows; keys of a range's sums
+    float *part;                    // [range][sequence][KV head][key]
 };
 __device__ __forceinline__ bool weigh_sees(const PagedWeigh &c, int pos, int key) {
     return key <= pos && (!c.window || pos - key < c.window || key < c.sinks);
@@ -94,6 +97,356 @@ __global__ __launch_bounds__(256) void k_weigh(PagedWeigh c) {
             *w = key < s.first ? *w + sum : sum;
         }
     }
+}
+
+// The same for sequences whose rows fit NB blocks of 16 (decode steps, catch-ups): bound by the reading of K, so K comes as whole lines, through a ring of tiles of 32 keys in
+// LDS that is the wave's own (no barrier), with the exponents and with the weights as they were; the rows' queries stay in registers.
+template <typename CT, int HD, int NB>
+struct WeighWave {
+    static constexpr bool F32 = sizeof(CT) == 4, F8 = sizeof(CT) == 1;
+    static constexpr int kRow = HD * (int)sizeof(CT), kKeys = 32 * kRow;      // bytes of a key, of a tile's keys
+    static constexpr int kReq = 16 * kRow / 1024 > 0 ? 16 * kRow / 1024 : 1;  // requests for 16 keys (8-bit HD 32: for 32)
+    static constexpr bool kShort = 16 * kRow < 1024;
+    static constexpr int kTile = kKeys + 256 + (F8 ? 256 : 0), kRequests = (kShort ? 1 : 2 * kReq) + 1 + (F8 ? 1 : 0);
+    static constexpr int kRing = kKeys >= 8192 ? 2 : 16384 / kKeys;           // tiles
+    static constexpr int KE = F32 ? 4 : F8 ? (HD >= 64 ? 16 : 8) : 8;         // neighbouring elements of K in one read
+    static constexpr int KL = HD / 4 / KE;                                    // reads per key
+    static constexpr int QW = F32 ? HD / 4 : HD / 8;                          // words of Q per lane
+};
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+constexpr int kWeighTiles = 32;      // tiles of 32 keys that a wave takes at most: their pages lie in its lanes
+
+template <typename CT, int HD, int NB>
+__global__ __launch_bounds__(256, 2) void k_weigh_few(PagedWeigh c) {
+    using W = WeighWave<CT, HD, NB>;
+    constexpr int kRow = W::kRow;
+    __shared__ __align__(1024) char lds[4 * W::kRing * W::kTile];
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int n = lane & 15, g = lane >> 4, h = (int)blockIdx.x % c.a.n_kv;
+    const PagedSeq s = paged_seq(c.a, blockIdx.y);
+    const int rows = min(s.n_rows * c.group, NB * 16);
+    const int key0 = ((int)blockIdx.x / c.a.n_kv * c.tiles * 4 + wave) * 32;       // this wave's tiles: every fourth from here
+    const int count = min((s.kv - key0 + 127) / 128, c.tiles);
+    if (rows <= 0 || count <= 0) return;
+    const int page_mask = (1 << c.a.page_shift) - 1;
+    int pages = -1;                                          // lane 2 i + half: keys 16 half .. of tile i
+    {
+        const int pos = key0 + (lane >> 1) * 128 + (lane & 1) * 16;
+        if ((lane >> 1) < count && pos < s.kv) pages = paged_page(c.a, s, pos);
+    }
+    // element KE (4 i + g) + .. of a row's queries belongs to K's read i: the contraction's order is free as long as both have the same
+    uint32_t q[NB][W::QW];
+    float nl[NB][4];                                         // -lse in bits of this lane's rows, -inf where there is none
+    int p_lo = s.first, p_hi = s.first + (rows - 1) / c.group;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int i = 0; i < W::QW; ++i) q[b][i] = 0u;
+        const int r = b * 16 + n, tok = r / c.group, qh = h * c.group + r % c.group;
+        if (r < rows) {
+            const size_t at = (size_t)(s.row0 + tok) * c.q.row_stride + (size_t)qh * c.q.head_stride;
+#pragma unroll
+            for (int i = 0; i < W::KL; ++i) {
+                const int d = (4 * i + g) * W::KE;
+                if constexpr (W::F32) {
+                    const float *p = (const float *)c.q.p + at + d;
+                    if (c.q.vec) { Raw<16> x; x.load(p); for (int e = 0; e < 4; ++e) q[b][i * 4 + e] = x.w[e]; }
+                    else for (int e = 0; e < 4; ++e) q[b][i * 4 + e] = __float_as_uint(p[e]);
+                } else {
+                    const bf16_t *p = (const bf16_t *)c.q.p + at + d;
+                    if (c.q.vec) { Raw<W::KE * 2> x; x.load(p); for (int e = 0; e < W::KE / 2; ++e) q[b][i * (W::KE / 2) + e] = x.w[e]; }
+                    else for (int e = 0; e < W::KE / 2; ++e) q[b][i * (W::KE / 2) + e] = (uint32_t)p[2 * e].u | (uint32_t)p[2 * e + 1].u << 16;
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int rr = b * 16 + 4 * g + e;
+            float z = -INFINITY;
+            if (rr < rows) z = c.lse[(size_t)(s.row0 + rr / c.group) * c.n_heads + h * c.group + rr % c.group];
+            nl[b][e] = z == -INFINITY ? -INFINITY : -1.4426950408889634f * z;
+        }
+    }
+    uint32_t from[W::kReq], k_at[W::KL];
+#pragma unroll
+    for (int e = 0; e < W::kReq; ++e) {                      // where this lane's piece of a request lies among 16 keys
+        const int at = e * 1024 + lane * 16, key = at / kRow, piece = at % kRow >> 4;
+        from[e] = (W::kShort ? key & 15 : key) * kRow + ((piece ^ lds_swizzle<kRow>(key)) << 4);
+    }
+    const uint32_t ring = lds_address(lds) + wave * W::kRing * W::kTile;
+#pragma unroll
+    for (int i = 0; i < W::KL; ++i) {
+        const int byte = (4 * i + g) * W::KE * (int)sizeof(CT);
+        k_at[i] = n * kRow + (((byte >> 4) ^ lds_swizzle<kRow>(n)) << 4) + (byte & 15);
+    }
+    // Requests a tile.  Every address is inside the pools: halves without a page read page 0, and nothing is kept of them
+    auto request = [&](int i) {
+        const int base = key0 + i * 128;
+        const int page0 = max(__builtin_amdgcn_readlane(pages, 2 * i), 0), page1 = max(__builtin_amdgcn_readlane(pages, 2 * i + 1), 0);
+        const size_t vec0 = scalar(paged_vec(c.a, page0, h, base & page_mask)), vec1 = scalar(paged_vec(c.a, page1, h, (base + 16) & page_mask));
+        const uint32_t to = __builtin_amdgcn_readfirstlane(ring + i % W::kRing * W::kTile);
+        if constexpr (W::kShort) {
+            request_pieces((const char *)c.a.k + (lane < 32 ? vec0 : vec1) * kRow + from[0], to);
+        } else {
+#pragma unroll
+            for (int e = 0; e < W::kReq; ++e) request_tile<true>((const bf16_t *)((const char *)c.a.k + vec0 * kRow), from[e], to + e * 1024);
+#pragma unroll
+            for (int e = 0; e < W::kReq; ++e) request_tile<true>((const bf16_t *)((const char *)c.a.k + vec1 * kRow), from[e], to + (W::kReq + e) * 1024);
+        }
+        request_words(c.weights + (lane & 16 ? vec1 : vec0) + (lane & 15), to + W::kKeys);        // lanes 0 .. 31: the tile's keys; the others repeat them
+        if constexpr (W::F8) request_words(c.a.ks + (lane & 4 ? vec1 : vec0) + 4 * (lane & 3), to + W::kKeys + 256);
+    };
+    auto take = [&](int i, auto edge_c) {
+        constexpr bool EDGE = decltype(edge_c)::value;
+        const int base = key0 + i * 128;
+        const uint32_t at = ring + i % W::kRing * W::kTile;
+        float sum[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const uint32_t keys = at + half * 16 * kRow;
+            f32x4_t sc[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            float f = 0.f;
+            if constexpr (W::F8) f = exp2_of((int)lds_read<uint8_t>(at + W::kKeys + 256 + half * 16 + n));
+#pragma unroll
+            for (int j = 0; j < W::KL; ++j) {
+                if constexpr (W::F32) {
+                    const f32x4e_t k = lds_read<f32x4e_t>(keys + k_at[j]);
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[b][j * 4 + e]), k[e], sc[b], 0, 0, 0);
+                } else {
+                    uint32_t w[W::KE / 2];
+                    if constexpr (!W::F8) { const u32x4_t x = lds_read<u32x4_t>(keys + k_at[j]); w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; }
+                    else if constexpr (W::KE == 16) {
+                        const u32x4_t x = lds_read<u32x4_t>(keys + k_at[j]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { w[2 * e] = fp8_bf16x2<false>(x[e], f); w[2 * e + 1] = fp8_bf16x2<true>(x[e], f); }
+                    } else {
+                        const u32x2_t x = lds_read<u32x2_t>(keys + k_at[j]);
+                        w[0] = fp8_bf16x2<false>(x.x, f); w[1] = fp8_bf16x2<true>(x.x, f); w[2] = fp8_bf16x2<false>(x.y, f); w[3] = fp8_bf16x2<true>(x.y, f);
+                    }
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int x = 0; x < W::KE / 8; ++x) {
+                            const uint32_t *p = q[b] + j * (W::KE / 2) + 4 * x;
+                            sc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{p[0], p[1], p[2], p[3]}),
+                                                                            __builtin_bit_cast(bf16x8_t, u32x4_t{w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]}), sc[b], 0, 0, 0);
+                        }
+                }
+            }
+            float t = 0.f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int rr = b * 16 + 4 * g + e;
+                    float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][e], c.c2, nl[b][e]));
+                    // a row that pays nothing does so to an infinite key too
+                    x = nl[b][e] == -INFINITY ? 0.f : x;
+                    if constexpr (EDGE) x = rr < rows && weigh_sees(c, s.first + rr / c.group, base + 16 * half + n) ? x : 0.f;
+                    t += x;
+                }
+            t += __shfl_xor(t, 16, kWave);
+            t += __shfl_xor(t, 32, kWave);
+            sum[half] = t;
+        }
+        // lanes 0 .. 15 have the first half's keys, 16 .. 31 the second's
+        const int key = base + (lane & 31), page = __builtin_amdgcn_readlane(pages, 2 * i), page_too = __builtin_amdgcn_readlane(pages, 2 * i + 1);
+        const int mine = lane & 16 ? page_too : page;
+        const float old = lds_read<float>(at + W::kKeys + 4 * (lane & 31));
+        if (lane < 32 && mine >= 0 && key < s.kv)
+            c.weights[paged_vec(c.a, mine, h, key & page_mask)] = (key < s.first ? old : 0.f) + (lane & 16 ? sum[1] : sum[0]);
+    };
+#pragma unroll
+    for (int i = 0; i < W::kRing - 1; ++i)
+        if (i < count) request(i);
+    for (int i = 0; i < count; ++i) {
+        if (i + W::kRing - 1 < count) {
+            request(i + W::kRing - 1);
+            wait_requests<(W::kRing - 1) * W::kRequests>();
+        } else wait_requests<0>();
+        const int base = key0 + i * 128, last = base + 31;
+        if (last <= p_lo && (!c.window || p_hi - base < c.window || last < c.sinks)) take(i, std::false_type{});
+        else take(i, std::true_type{});
+    }
+}
+
+// Many rows (prompts and pieces of them): bound by products and exponentials, so the keys stay in registers, 64 to a wave and 256 to a workgroup, and the rows come
+// through LDS, 32 at a time, requested one tile ahead and read by all four waves.
+//   S = Q K^T with 32x32x16 products: lane (n, hh) = (lane & 31, lane >> 5) gets key n's scores of rows 8 i + 4 hh + 0..3 of a tile, i = 0..3, and adds their
+//   exponentials up; the halves of the wave are added at the end.
+// The rows that see a tile of keys are cut into c.splits ranges; with more than one each leaves its sums for k_weigh_join.
+template <typename CT, int HD>
+__global__ __launch_bounds__(256, 2) void k_weigh_many(PagedWeigh c) {
+    constexpr int KS = HD / 16, kRowBytes = HD * 2, kTileBytes = 32 * kRowBytes, kReq = kTileBytes / 4096;     // requests of 1 KB to a wave (HD 32: half a one)
+    __shared__ __align__(1024) char lds[2 * kTileBytes];
+    __shared__ __align__(16) float nls[2][32];               // -lse in bits, -inf where a row pays nothing
+    __shared__ int odd[2];                                   // whether there is such a row
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int n = lane & 31, hh = lane >> 5;
+    const int h = (int)blockIdx.x % c.a.n_kv, rest = (int)blockIdx.x / c.a.n_kv, split = rest % c.splits, key0 = rest / c.splits * 256, my0 = key0 + wave * 64;
+    const PagedSeq s = paged_seq(c.a, blockIdx.y);
+    const int rows = s.n_rows * c.group;
+    if (rows == 0 || key0 >= s.kv) return;
+    // tiles of rows that see any of the workgroup's keys, and this range's of them
+    const int last_key = min(key0 + 255, s.kv - 1);
+    int t0 = max(key0 - s.first, 0) * c.group / 32, t1 = (rows + 31) / 32;
+    if (c.window && key0 >= c.sinks) t1 = (int)min((long)t1, max(((long)last_key + c.window - s.first) * c.group + 31, 0l) / 32);
+    const int per = max((t1 - t0 + c.splits - 1) / c.splits, 0);
+    t0 += split * per;
+    t1 = min(t1, t0 + per);
+    const int page_mask = (1 << c.a.page_shift) - 1;
+    size_t vec[2];
+    bool live[2];
+    bf16x8_t k[2][KS];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int key = my0 + 32 * b + n, page = key < s.kv ? paged_page(c.a, s, key) : -1;
+        live[b] = page >= 0;
+        vec[b] = paged_vec(c.a, max(page, 0), h, key & page_mask);
+        const float f = sizeof(CT) == 1 ? exp2_of(c.a.ks[vec[b]]) : 0.f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            const int d = 16 * i + 8 * hh;
+            if constexpr (sizeof(CT) == 1) {
+                const u32x2_t w = *(gptr<u32x2_t>)((const uint8_t *)c.a.k + vec[b] * HD + d);
+                k[b][i] = __builtin_bit_cast(bf16x8_t, u32x4_t{fp8_bf16x2<false>(w.x, f), fp8_bf16x2<true>(w.x, f), fp8_bf16x2<false>(w.y, f), fp8_bf16x2<true>(w.y, f)});
+            } else k[b][i] = __builtin_bit_cast(bf16x8_t, *(gptr<u32x4_t>)((const bf16_t *)c.a.k + vec[b] * HD + d));
+        }
+    }
+    // ---- staging: a request is 16 bytes to a lane; this lane's pieces of a tile belong to rows r_of[e], which advance by 32 rows a tile without a division
+    const uint32_t base = lds_address(lds);
+    constexpr int kPieces = kReq > 0 ? kReq : 1;
+    const bool asks = kReq > 0 || wave < 2;
+    int tok[kPieces], rem[kPieces], piece[kPieces], row_at[kPieces];
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+        const int at = (kReq > 0 ? wave * kReq + e : wave & 1) * 1024 + lane * 16, r = at / kRowBytes;
+        piece[e] = ((at % kRowBytes >> 4) ^ lds_swizzle<kRowBytes>(r)) * 8;
+        row_at[e] = t0 * 32 + r;
+        tok[e] = row_at[e] / c.group;
+        rem[e] = row_at[e] % c.group;
+    }
+    const int step_tok = 32 / c.group, step_rem = 32 % c.group;
+    int z_row = t0 * 32 + lane, z_tok = z_row / c.group, z_rem = z_row % c.group;          // wave 0, lanes 0 .. 31: the tile's lse
+    auto request = [&](int t) {
+        const uint32_t to = __builtin_amdgcn_readfirstlane(base + (t & 1) * kTileBytes + (kReq > 0 ? wave * kReq : wave & 1) * 1024);
+        if (!asks) return;
+#pragma unroll
+        for (int e = 0; e < kPieces; ++e) {
+            const bool in = row_at[e] < rows;                // past the last row: the first one, whose scores are left out
+            const size_t at = (size_t)(s.row0 + (in ? tok[e] : 0)) * c.q.row_stride + (size_t)(h * c.group + (in ? rem[e] : 0)) * c.q.head_stride;
+            request_pieces((const bf16_t *)c.q.p + at + piece[e], to + e * 1024);
+            row_at[e] += 32;
+            tok[e] += step_tok;
+            rem[e] += step_rem;
+            if (rem[e] >= c.group) { rem[e] -= c.group; ++tok[e]; }
+        }
+    };
+    auto next_lse = [&] {
+        float z = -INFINITY;
+        if (wave == 0 && lane < 32 && z_row < rows) z = c.lse[(size_t)(s.row0 + z_tok) * c.n_heads + h * c.group + z_rem];
+        z_row += 32;
+        z_tok += step_tok;
+        z_rem += step_rem;
+        if (z_rem >= c.group) { z_rem -= c.group; ++z_tok; }
+        return z;
+    };
+    auto put_lse = [&](int t, float z) {
+        if (wave) return;
+        const uint64_t none = __ballot(lane < 32 && z == -INFINITY);
+        if (lane < 32) nls[t & 1][lane] = z == -INFINITY ? -INFINITY : -1.4426950408889634f * z;
+        if (lane == 0) odd[t & 1] = none != 0;
+    };
+    const uint32_t q_at = base + n * kRowBytes + ((hh ^ lds_swizzle<kRowBytes>(n)) << 4);
+    float sum[2] = {0.f, 0.f};
+    int p_tok = t0 * 32 / c.group, p_rem = t0 * 32 % c.group;                              // the tile's first row
+    auto take = [&](int t, auto edge_c) {
+        constexpr bool EDGE = decltype(edge_c)::value;
+        f32x16_t sc[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            const bf16x8_t q = *(__attribute__((address_space(3))) bf16x8_t *)(uintptr_t)((q_at ^ (32 * i)) + (t & 1) * kTileBytes);
+            sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[0][i], sc[0], 0, 0, 0);
+            sc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[1][i], sc[1], 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4e_t nl = *(const f32x4e_t *)&nls[t & 1][8 * i + 4 * hh];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                int pos = 0;
+                bool pays = true;
+                if constexpr (EDGE) {
+                    const int r = t * 32 + 8 * i + 4 * hh + e;
+                    pos = s.first + r / c.group;
+                    pays = r < rows && nl[e] != -INFINITY;
+                }
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][4 * i + e], c.c2, nl[e]));
+                    if constexpr (EDGE) x = pays && weigh_sees(c, pos, my0 + 32 * b + n) ? x : 0.f;
+                    sum[b] += x;
+                }
+            }
+        }
+    };
+    if (t0 < t1) {
+        const float first = next_lse();
+        request(t0);
+        put_lse(t0, first);
+        for (int t = t0; t < t1; ++t) {
+            wait_requests<0>();
+            __syncthreads();
+            float coming = 0.f;
+            if (t + 1 < t1) {
+                coming = next_lse();
+                request(t + 1);
+            }
+            const int p_lo = s.first + p_tok;
+            p_tok += step_tok;
+            p_rem += step_rem;
+            if (p_rem >= c.group) { p_rem -= c.group; ++p_tok; }
+            const int p_next = s.first + p_tok;              // no row of this tile is past the next one's first
+            if (p_next >= my0) {
+                if (my0 + 63 <= p_lo && !odd[t & 1] && (!c.window || p_next - my0 < c.window || my0 + 63 < c.sinks)) take(t, std::false_type{});
+                else take(t, std::true_type{});
+            }
+            if (t + 1 < t1) put_lse(t + 1, coming);
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        sum[b] += __shfl_xor(sum[b], 32, kWave);
+        const int key = my0 + 32 * b + n;
+        if (hh == 0 && live[b]) {
+            if (c.splits > 1) c.part[(((size_t)split * gridDim.y + blockIdx.y) * c.a.n_kv + h) * c.part_keys + key] = sum[b];
+            else c.weights[vec[b]] = (key < s.first ? c.weights[vec[b]] : 0.f) + sum[b];
+        }
+    }
+}
+
+// The ranges' sums of a position, in their order, on top of what it had
+__global__ __launch_bounds__(256) void k_weigh_join(PagedWeigh c) {
+    const int h = (int)blockIdx.y, key = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    const PagedSeq s = paged_seq(c.a, blockIdx.z);
+    if (s.n_rows == 0 || key >= min(s.kv, c.part_keys)) return;
+    const int page = paged_page(c.a, s, key);
+    if (page < 0) return;
+    float *w = c.weights + paged_vec(c.a, page, h, key & ((1 << c.a.page_shift) - 1));
+    float sum = key < s.first ? *w : 0.f;
+    const size_t apart = (size_t)gridDim.z * c.a.n_kv * c.part_keys;
+    const float *p = c.part + ((size_t)blockIdx.z * c.a.n_kv + h) * c.part_keys + key;
+    for (int i = 0; i < c.splits; ++i) sum += p[i * apart];
+    *w = sum;
 }
 
 }  // namespace ead
