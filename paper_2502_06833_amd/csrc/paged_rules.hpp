@@ -105,12 +105,13 @@ inline PagedPlan paged_many(int batch, int n_kv, int group, long rows, int max_k
     return paged_cut(128, 64, rows, batch, n_kv, group, max_kv, window, sinks, 2l * cus, 4, paged_many_splits(head_dim));
 }
 
-// Groups of lanes that share a row of queries, keys (and values) whose heads are normalised and turned: a head to each while the rows do not fill the device, then fewer,
-// which compute a row's sines and cosines less often.
-inline int rotate_groups(long rows, int heads, int head_dim) {
-    const long lanes = rows * heads * (head_dim / 16), each = std::max(1l, lanes / (256l * 2048));
-    return (int)std::max(1l, (heads + each - 1) / each);
-}
+// ---- rotation ----
+// Heads of a row that a group of lanes takes: one while that does not fill the device, then four, which share sines and cosines and are requested together
+constexpr int kRotateEach = 4;
+inline bool rotate_wide(long rows, long heads, int head_dim) { return rows * heads * (head_dim / 16) > 4l * 256 * 1024; }
+inline long rotate_units(long q, long k, long v, int each) { return (q + each - 1) / each + (k + each - 1) / each + (v + each - 1) / each; }
+// Whether a call moves more than stays in the second-level caches
+inline bool rotate_streams(long rows, long heads, int head_dim, int bytes) { return 2.0 * rows * heads * head_dim * bytes > 64e6; }
 
 // ---- weighing ----
 // Sequences of up to this many rows per KV head (new tokens times query heads per KV head) keep their queries in registers while keys stream past (k_weigh_few); with more

@@ -13,7 +13,7 @@ struct RotateArgs {
     long q_gain_stride, k_gain_stride;   // from head to head, 0: one gain for all
     float eps;
     int n_heads, n_kv, rotary, interleaved;
-    int groups;                          // groups of lanes that share a row
+    int groups;                          // units of a row's heads (rotate_unit)
 };
 
 // Sine and cosine of a quarter turn's fraction: |r| <= 1/2, the angle r pi / 2 is at most pi / 4 in magnitude, where the Taylor series up to x^9 and x^10 are off by
@@ -88,7 +88,7 @@ __device__ __forceinline__ void norm_turn(float (&x)[8], float (&y)[8], const fl
 }
 
 // The sixteen elements of this lane to the cache, rounded to its type (as put8 in paged.hpp, which has eight to a lane)
-template <typename CT, int HD>
+template <typename CT, int HD, bool STREAM>
 __device__ __forceinline__ void put16(void *pool, uint8_t *scales, size_t vec, int lane, const RotateLane &l, float (&x)[8], float (&y)[8], bool live) {
     if constexpr (sizeof(CT) == 1) {
         float m = 0.f;
@@ -108,80 +108,122 @@ __device__ __forceinline__ void put16(void *pool, uint8_t *scales, size_t vec, i
             y[e] = __builtin_fabsf(y[e]) <= 3.402823466e38f ? y[e] * inv : __builtin_nanf("");
         }
         if (live) {
-            *(u32x2_t *)((uint8_t *)pool + vec * HD + l.at) = u32x2_t{fp8_pack4(x[0], x[1], x[2], x[3]), fp8_pack4(x[4], x[5], x[6], x[7])};
-            *(u32x2_t *)((uint8_t *)pool + vec * HD + l.too) = u32x2_t{fp8_pack4(y[0], y[1], y[2], y[3]), fp8_pack4(y[4], y[5], y[6], y[7])};
+            put<STREAM>((u32x2_t *)((uint8_t *)pool + vec * HD + l.at), u32x2_t{fp8_pack4(x[0], x[1], x[2], x[3]), fp8_pack4(x[4], x[5], x[6], x[7])});
+            put<STREAM>((u32x2_t *)((uint8_t *)pool + vec * HD + l.too), u32x2_t{fp8_pack4(y[0], y[1], y[2], y[3]), fp8_pack4(y[4], y[5], y[6], y[7])});
             if (lane == 0) scales[vec] = (uint8_t)ex;
         }
     } else if (live) {
-        set8<false>((CT *)pool + vec * HD + l.at, 1, x);
-        set8<false>((CT *)pool + vec * HD + l.too, 1, y);
+        set8<STREAM>((CT *)pool + vec * HD + l.at, 1, x);
+        set8<STREAM>((CT *)pool + vec * HD + l.too, 1, y);
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void rotate_gains(const float *gain, long stride, int h, const RotateLane &l, float (&gx)[8], float (&gy)[8]) {
-    if (!gain) return;
-    const float *p = gain + h * stride;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) { gx[e] = p[l.at + e]; gy[e] = p[l.too + e]; }
+// A group of HD / 16 lanes takes EACH heads of one kind (queries, keys, or values on their way to the pages) of a row, all of them requested before the first is worked
+// on; the row's sines and cosines are computed once for them, meanwhile.
+struct RotateUnit {
+    int kind, first, heads;              // 0: queries, 1: keys, 2: values; heads first .. first + heads - 1
+};
+template <int EACH>
+__device__ __forceinline__ RotateUnit rotate_unit(const RotateArgs &c, int u) {
+    const int uq = (c.n_heads + EACH - 1) / EACH, uk = (c.n_kv + EACH - 1) / EACH;
+    RotateUnit r;
+    r.kind = u < uq ? 0 : u < uq + uk ? 1 : 2;
+    r.first = (u - (r.kind == 0 ? 0 : r.kind == 1 ? uq : uq + uk)) * EACH;
+    r.heads = min(EACH, (r.kind == 0 ? c.n_heads : c.n_kv) - r.first);
+    return r;
 }
 
-// A group of HD / 16 lanes takes a row's vectors g, g + groups, ...: query heads, then key heads, then (APPEND) value heads, with sines and cosines computed once.
-template <typename CT, typename RT, int HD, bool APPEND>
-__device__ __forceinline__ void rotate_row(const RotateArgs &c, size_t row, int position, int g, int lane, const RotateLane &l, size_t page_vec, bool live) {
-    float sn[8] = {}, cs[8] = {};
-    if (l.turns) {
+// Eight elements at any alignment
+__device__ __forceinline__ void rotate_gather(Vec8<float> &v, const float *p) {
+    v.lo = f32x4e_t{p[0], p[1], p[2], p[3]};
+    v.hi = f32x4e_t{p[4], p[5], p[6], p[7]};
+}
+__device__ __forceinline__ void rotate_gather(Vec8<bf16_t> &v, const bf16_t *p) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v.raw[e] = (uint32_t)p[2 * e].u | (uint32_t)p[2 * e + 1].u << 16;
+}
+
+template <typename CT, typename RT, int HD, int EACH, bool STREAM, bool APPEND>
+__device__ __forceinline__ void rotate_row(const RotateArgs &c, const RotateUnit &u, size_t row, int position, int lane, const RotateLane &l, size_t page_vec, bool live) {
+    const RowsArg &from = u.kind == 0 ? c.q : u.kind == 1 ? c.k : c.v;
+    const RT *p = (const RT *)from.p + row * from.row_stride + u.first * from.head_stride;
+    // (as they lie in memory, and without a branch between them: unpacked one by one they were waited for one by one)
+    Vec8<RT> rx[EACH], ry[EACH];
+    if (from.vec) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const RT *v = p + min(e, u.heads - 1) * from.head_stride;
+            if constexpr (STREAM) { rx[e].load_stream(v + l.at); ry[e].load_stream(v + l.too); }
+            else { rx[e].load(v + l.at); ry[e].load(v + l.too); }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const RT *v = p + min(e, u.heads - 1) * from.head_stride;
+            rotate_gather(rx[e], v + l.at);
+            rotate_gather(ry[e], v + l.too);
+        }
+    }
+    const float *gain = u.kind == 0 ? c.q_gain : u.kind == 1 ? c.k_gain : nullptr;
+    const long apart = u.kind == 0 ? c.q_gain_stride : c.k_gain_stride;
+    float gx[8] = {}, gy[8] = {}, sn[8] = {}, cs[8] = {};
+    auto gains = [&](int h) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { gx[e] = gain[h * apart + l.at + e]; gy[e] = gain[h * apart + l.too + e]; }
+    };
+    if (gain && !apart) gains(0);
+    const bool turns = l.turns && u.kind < 2;
+    if (turns) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) sincos_of((double)position, c.inv_freq[8 * lane + e], sn[e], cs[e]);
     }
-    const int total = c.n_heads + (APPEND ? 2 : 1) * c.n_kv;
-    for (int i = g; i < total; i += c.groups) {
-        const int kind = i < c.n_heads ? 0 : i < c.n_heads + c.n_kv ? 1 : 2, h = kind == 0 ? i : kind == 1 ? i - c.n_heads : i - c.n_heads - c.n_kv;
-        const RowsArg &from = kind == 0 ? c.q : kind == 1 ? c.k : c.v;
-        const RT *p = (const RT *)from.p + row * from.row_stride + h * from.head_stride;
-        float x[8], y[8], gx[8] = {}, gy[8] = {};
-        load8<false>(p + l.at, from.vec, x);
-        load8<false>(p + l.too, from.vec, y);
-        const float *gain = kind == 0 ? c.q_gain : kind == 1 ? c.k_gain : nullptr;
-        rotate_gains<float>(gain, kind == 0 ? c.q_gain_stride : c.k_gain_stride, h, l, gx, gy);
-        norm_turn<HD>(x, y, gx, gy, gain != nullptr, c.eps, l.turns && kind < 2, c.interleaved, sn, cs);
-        if (kind == 0 || !APPEND) {
-            const RowsArg &to = kind == 0 ? c.q_out : c.k_out;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        if (e >= u.heads) continue;
+        const int h = u.first + e;
+        float x[8], y[8];
+        rx[e].unpack(x);
+        ry[e].unpack(y);
+        if (gain && apart) gains(h);
+        norm_turn<HD>(x, y, gx, gy, gain != nullptr, c.eps, turns, c.interleaved, sn, cs);
+        if (u.kind == 0 || !APPEND) {
+            const RowsArg &to = u.kind == 0 ? c.q_out : c.k_out;
             RT *o = (RT *)to.p + row * to.row_stride + h * to.head_stride;
-            set8<false>(o + l.at, to.vec, x);
-            set8<false>(o + l.too, to.vec, y);
+            set8<STREAM>(o + l.at, to.vec, x);
+            set8<STREAM>(o + l.too, to.vec, y);
         } else {
-            put16<CT, HD>((void *)(kind == 1 ? c.a.k : c.a.v), (uint8_t *)(kind == 1 ? c.a.ks : c.a.vs), page_vec + ((size_t)h << c.a.page_shift), lane, l, x, y, live);
+            put16<CT, HD, STREAM>((void *)(u.kind == 1 ? c.a.k : c.a.v), (uint8_t *)(u.kind == 1 ? c.a.ks : c.a.vs), page_vec + ((size_t)h << c.a.page_shift), lane, l, x, y, live);
         }
     }
 }
 
-template <typename RT, int HD>
+template <typename RT, int HD, int EACH, bool STREAM>
 __global__ __launch_bounds__(256) void k_rotate(RotateArgs c) {
     constexpr int L = HD / 16, kGroups = 256 / L;
     const int lane = (int)threadIdx.x % L;
     const RotateLane l = rotate_lane(lane, c.rotary, c.interleaved);
-    const long total = (long)c.a.rows * c.groups;
-    for (long i = (long)blockIdx.x * kGroups + (int)threadIdx.x / L; i < total; i += (long)gridDim.x * kGroups) {
-        const size_t row = (size_t)(i / c.groups);
-        rotate_row<RT, RT, HD, false>(c, row, c.positions[row], (int)(i % c.groups), lane, l, 0, false);
+    const unsigned total = (unsigned)c.a.rows * (unsigned)c.groups;            // below 2^30
+    for (unsigned i = blockIdx.x * kGroups + threadIdx.x / L; i < total; i += gridDim.x * kGroups) {
+        const unsigned row = i / (unsigned)c.groups;
+        rotate_row<RT, RT, HD, EACH, STREAM, false>(c, rotate_unit<EACH>(c, (int)(i % (unsigned)c.groups)), row, c.positions ? c.positions[row] : 0, lane, l, 0, false);
     }
 }
 
 // Rows of no sequence are not touched; keys and values of rows below position 0, past the table or in holes go nowhere.
-template <typename CT, typename RT, int HD>
+template <typename CT, typename RT, int HD, int EACH, bool STREAM>
 __global__ __launch_bounds__(256) void k_append(RotateArgs c) {
     constexpr int L = HD / 16, kGroups = 256 / L;
     const int lane = (int)threadIdx.x % L;
     const RotateLane l = rotate_lane(lane, c.rotary, c.interleaved);
     const PagedSeq s = paged_seq(c.a, blockIdx.y);
-    const long total = (long)s.n_rows * c.groups;
-    for (long i = (long)blockIdx.x * kGroups + (int)threadIdx.x / L; i < total; i += (long)gridDim.x * kGroups) {
-        const int t = (int)(i / c.groups), pos = s.first + t;
+    const unsigned total = (unsigned)s.n_rows * (unsigned)c.groups;
+    for (unsigned i = blockIdx.x * kGroups + threadIdx.x / L; i < total; i += gridDim.x * kGroups) {
+        const int t = (int)(i / (unsigned)c.groups), pos = s.first + t;
+        const RotateUnit u = rotate_unit<EACH>(c, (int)(i % (unsigned)c.groups));
         const size_t row = (size_t)(s.row0 + t);
-        const int page = pos >= 0 && pos < s.kv ? paged_page(c.a, s, pos) : -1;
+        const int page = u.kind && pos >= 0 && pos < s.kv ? paged_page(c.a, s, pos) : -1;
         const size_t vec = paged_vec(c.a, max(page, 0), 0, pos & ((1 << c.a.page_shift) - 1));
-        rotate_row<CT, RT, HD, true>(c, row, c.positions ? c.positions[row] : pos, (int)(i % c.groups), lane, l, vec, page >= 0);
+        rotate_row<CT, RT, HD, EACH, STREAM, true>(c, u, row, c.positions ? c.positions[row] : pos, lane, l, vec, page >= 0);
     }
 }
 
