@@ -24,7 +24,7 @@ struct LogprobArgs {
     float *top_logprobs;
     int *tickets;                             // parts > 1: [row], zero between launches
     LpPartial *stats;                         // [row][part]
-    float *list_value;                        // [row][part][top]
+    float *list_value;                        // [row][place][part]: neighbours are of one place, so that the bound of the join is a good one
     int *list_token;
 };
 
@@ -140,43 +140,41 @@ struct LpRow {
 };
 
 // ---- the most likely tokens ----------------------------------------------------------------------
-// While the sums are taken each lane only notes the largest logit of every group of its sets.  The k-th largest of 64 disjoint parts' largest logits (the four waves' lanes,
-// lane by lane) is a bound from below for the k-th largest logit, and hardly more than k logits reach it: the groups that do are read again, what reaches the bound is
-// collected, and each collected logit's place is the number of those before it.  Where more than 64 reach it (many equal logits) the row is gone through once more with
-// a list that is kept sorted (LpList).
-struct LpCollect {
-    float bound;
-    int count, groups[4];                     // collected; groups of a wave
-    float v[64];
-    int t[64];
-};
-
-// The k-th largest of 64 lanes' values, -inf where fewer are above that
-template <bool HALF> __device__ __forceinline__ float lp_kth(float v, int k) {
-    const uint32_t key = lp_rank(v);
+// While the sums are taken each lane only notes the largest logit of every group of its sets.  The k-th largest of 128 disjoint parts' largest logits (two waves' lanes
+// together, lane by lane) is a bound from below for the k-th largest logit, and few more than k logits reach it (37 expected where k is 32): the groups that do are read
+// again, what reaches the bound is collected, and each collected logit's place is the number of those before it.  Where more than 64 reach it (many equal logits) the row
+// is gone through once more with a list that is kept sorted (LpList).
+// The k-th largest of 128 values, two to a lane, -inf where fewer are above that.  HALF: of bf16 values, whose lower halves are 0 (or all ones below 0, which a bound need
+// not have)
+template <bool HALF> __device__ __forceinline__ float lp_kth(float v, float w, int k) {
+    const uint32_t kv = lp_rank(v), kw = lp_rank(w);
     uint32_t t = 0;
-    for (int bit = 31; bit >= (HALF ? 16 : 0); --bit)                     // bf16 values: the lower halves are 0 (or all ones below 0, which the bound need not have)
-        if (__popcll(__ballot(key >= (t | 1u << bit))) >= k) t |= 1u << bit;
+    for (int bit = 31; bit >= (HALF ? 16 : 0); --bit) {
+        const uint32_t tried = t | 1u << bit;
+        if (__popcll(__ballot(kv >= tried)) + __popcll(__ballot(kw >= tried)) >= k) t = tried;
+    }
     const float f = lp_value(t);
     return f == f ? f : -INFINITY;
 }
-__device__ __forceinline__ void lp_collect(LpCollect &c, float v, int t, bool is, int lane) {
+// A wave's collected logits: the n-th to its n-th place; 64 at most are kept, and counted on
+struct LpCollect {
+    float v[64];
+    int t[64];
+};
+__device__ __forceinline__ void lp_collect(LpCollect &c, int &n, float v, int t, bool is, int lane) {
     const uint64_t hit = __ballot(is);
     if (!hit) return;
-    int at = 0;
-    if (lane == __builtin_ctzll(hit)) at = atomicAdd(&c.count, __popcll(hit));
-    at = __shfl(at, __builtin_ctzll(hit), kWave) + __popcll(hit & ((1ull << lane) - 1));
+    const int at = n + __popcll(hit & ((1ull << lane) - 1));
     if (is && at < 64) { c.v[at] = v; c.t[at] = t; }
+    n += __popcll(hit);
 }
-// Lane i's collected logit and its place among them (64 and more: there is none)
-__device__ __forceinline__ int lp_place(const LpCollect &c, int n, int lane, float &v, int &t) {
-    v = lane < n ? c.v[lane] : -INFINITY;
-    t = lane < n ? c.t[lane] : kNoIndex;
+// The place of a lane's logit among the first n lanes' (64 for the others): larger ones first, of equal ones the lower token
+__device__ __forceinline__ int lp_place(float v, int t, int n, int lane) {
+    const uint64_t key = (uint64_t)lp_rank(v + 0.f) << 32 | (uint32_t)~t;
     int place = 0;
     for (int j = 0; j < n; ++j) {
-        const float ov = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), j));
-        const int ot = __builtin_amdgcn_readlane(t, j);
-        place += ov > v || (ov == v && ot < t);
+        const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, j);
+        place += other > key;
     }
     return lane < n ? place : 64;
 }
@@ -186,17 +184,22 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
     __shared__ float s_m[4], s_Z[4], s_S[4];
     __shared__ int s_above[4], s_last;
     __shared__ float s_best[TOP ? 4 : 1][TOP ? kLpSlots : 1][64], s_lv[TOP ? 4 : 1][kTopMost];
+    __shared__ float s_lane[TOP ? 4 : 1][64];
     __shared__ int s_group[TOP ? 4 : 1][64], s_lt[TOP ? 4 : 1][kTopMost];
-    __shared__ LpCollect s_c;
+    __shared__ LpCollect s_c[TOP ? 4 : 1];
+    __shared__ int s_n[4];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int r = (int)blockIdx.x / a.parts, part = (int)blockIdx.x % a.parts;
     const LpRow<T> row(a, r);
-    const int token = a.tokens ? __builtin_amdgcn_readfirstlane(a.tokens[r]) : -1;
-    const bool given = token >= 0 && token < a.V;
-    const float mine = given ? to_f32(row.row[token]) : INFINITY;
     const int begin = part * a.part_sets + wave, end = min((row.vecs + kSet - 1) / kSet, (part + 1) * a.part_sets);
     const int sets = begin < end ? (end - begin + 3) / 4 : 0, each = (sets + kLpSlots - 1) / kLpSlots;       // this wave's: begin, begin + 4, ...; of a group
 
+    Vec8<T> A[kSetVecs], B[kSetVecs];
+    if (sets > 0) row.load(A, begin, lane);
+    if (sets > 1) row.load(B, begin + 4, lane);
+    const int token = a.tokens ? __builtin_amdgcn_readfirstlane(a.tokens[r]) : -1;
+    const bool given = token >= 0 && token < a.V;
+    const float mine = given ? to_f32(row.row[token]) : INFINITY;
     LpRun run;
     run.init();
     int above = 0, of_group = 0, slot = 0;
@@ -236,17 +239,11 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
             }
         }
     };
-    Vec8<T> A[kSetVecs], B[kSetVecs];
-    int set = begin;
-    if (set < end) row.load(A, set, lane);
-    while (set < end) {
-        const int next = set + 4;
-        if (next < end) row.load(B, next, lane);
+    for (int set = begin; set < end; set += 8) {               // one in hand, the next on its way
         take(A);
-        if (next >= end) break;
-        set = next + 4;
-        if (set < end) row.load(A, set, lane);
-        take(B);
+        if (set + 8 < end) row.load(A, set + 8, lane);
+        if (set + 4 < end) take(B);
+        if (set + 12 < end) row.load(B, set + 12, lane);
     }
     if (TOP && of_group) s_best[wave][slot++][lane] = best;
 
@@ -258,21 +255,32 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
     if (lane == 0) { s_m[wave] = wm; s_Z[wave] = run.Z; s_S[wave] = run.S; s_above[wave] = above; }
     LpList list;
     list.init();
-    int place = 64, top_t = kNoIndex;                          // wave 0: this lane's token and its place among the most likely, once they are known
+    int place = 64, top_t = kNoIndex, collected = 0;                          // wave 0: this lane's token and its place among the most likely, once they are known
     float top_v = -INFINITY;
     if constexpr (TOP) {
-        float *lanes = &s_lv[0][0];                            // (64 of its 128 places at a time: the waves' lanes' largest, joined by the first)
-        static_assert(4 * kTopMost >= 64, "");
-        if (threadIdx.x == 0) s_c.count = 0;
-        if (threadIdx.x < 64) lanes[lane] = lane_best;
+        s_lane[wave][lane] = lane_best;
         __syncthreads();
-        for (int w = 1; w < 4; ++w) {
-            if (wave == w) lanes[lane] = fmaxf(lanes[lane], lane_best);
-            __syncthreads();
-        }
-        const float bound = lp_kth<sizeof(T) == 2>(lanes[lane], a.top);
-        // this wave's groups that reach the bound
+        const float bound = lp_kth<sizeof(T) == 2>(fmaxf(s_lane[0][lane], s_lane[1][lane]), fmaxf(s_lane[2][lane], s_lane[3][lane]), a.top);
+        int found = 0;
+        auto collect = [&](const Vec8<T> (&s)[kSetVecs], int first_vec, bool in) {
+#pragma unroll
+            for (int i = 0; i < kSetVecs; ++i) {
+                float f[8];
+                s[i].unpack(f);
+                const float top = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+                if (!__any(in && top >= bound)) continue;
+                const int first = (first_vec + i * 64) * 8 - row.shift;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) lp_collect(s_c[wave], found, f[e], first + e, in && f[e] >= bound && f[e] > -INFINITY, lane);
+            }
+        };
+        // this wave's groups that reach the bound; two sets are still in registers
         int n = 0;
+        if (sets <= 2) {
+            slot = 0;
+            if (sets > 0) collect(A, begin * kSet + lane, true);
+            if (sets > 1) collect(B, (begin + 4) * kSet + lane, true);
+        }
         for (int i = 0; i < slot; ++i) {
             const float b = s_best[wave][i][lane];
             const uint64_t hit = __ballot(b >= bound && b > -INFINITY);
@@ -281,7 +289,7 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
             if ((hit >> lane & 1) && at < 64) s_group[wave][at] = i * 64 + lane;
             n += __popcll(hit);
         }
-        if (n > 64 && lane == 0) atomicAdd(&s_c.count, 1 << 20);
+        if (n > 64) found = 65;
         if (n <= 64 && n > 0) {
             const int id = lane < n ? s_group[wave][lane] : 0;
             for (int j = 0; j < each; ++j) {
@@ -292,21 +300,13 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
                     s[i].zero();
                     if (lane < n && at < sets) row.load_one(s[i], (begin + 4 * at) * kSet + i * 64 + (id & 63));
                 }
-#pragma unroll
-                for (int i = 0; i < kSetVecs; ++i) {
-                    float f[8];
-                    s[i].unpack(f);
-                    const float top = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
-                    const bool in = lane < n && at < sets;
-                    if (!__any(in && top >= bound)) continue;
-                    const int first = ((begin + 4 * at) * kSet + i * 64 + (id & 63)) * 8 - row.shift;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) lp_collect(s_c, f[e], first + e, in && f[e] >= bound && f[e] > -INFINITY, lane);
-                }
+                collect(s, (begin + 4 * at) * kSet + (id & 63), lane < n && at < sets);
             }
         }
+        if (lane == 0) s_n[wave] = found;
         __syncthreads();
-        if (s_c.count > 64) {                                  // this wave's sets once more, with a sorted list
+        collected = s_n[0] + s_n[1] + s_n[2] + s_n[3];
+        if (collected > 64) {                                  // this wave's sets once more, with a sorted list
             for (int at = begin; at < end; at += 4) {
                 row.load(A, at, lane);
 #pragma unroll
@@ -333,7 +333,13 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
         run.m = s_m[0]; run.Z = s_Z[0]; run.S = s_S[0]; run.above = s_above[0];
         for (int w = 1; w < 4; ++w) { LpRun o; o.m = s_m[w]; o.Z = s_Z[w]; o.S = s_S[w]; o.above = s_above[w]; run.add(o); }
         if constexpr (TOP) {
-            if (s_c.count <= 64) { place = lp_place(s_c, s_c.count, lane, top_v, top_t); return; }
+            if (collected <= 64) {
+                int w = 0, at = lane;
+                while (w < 3 && at >= s_n[w]) at -= s_n[w++];
+                if (lane < collected) { top_v = s_c[w].v[at]; top_t = s_c[w].t[at]; }
+                place = lp_place(top_v, top_t, collected, lane);
+                return;
+            }
             list.v = lane < kTopMost ? s_lv[0][lane] : -INFINITY;
             list.t = lane < kTopMost ? s_lt[0][lane] : kNoIndex;
             for (int w = 1; w < 4; ++w) {
@@ -353,8 +359,9 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
             }
             if constexpr (TOP) {
                 const int have = __popcll(__ballot(place < a.top));
-                if (place < a.top) { st_coherent(a.list_value + at * a.top + place, top_v); st_coherent(a.list_token + at * a.top + place, top_t); }
-                if (lane >= have && lane < a.top) { st_coherent(a.list_value + at * a.top + lane, -INFINITY); st_coherent(a.list_token + at * a.top + lane, kNoIndex); }
+                const size_t to = (size_t)r * a.parts * a.top + part;
+                if (place < a.top) { st_coherent(a.list_value + to + place * a.parts, top_v); st_coherent(a.list_token + to + place * a.parts, top_t); }
+                if (lane >= have && lane < a.top) { st_coherent(a.list_value + to + lane * a.parts, -INFINITY); st_coherent(a.list_token + to + lane * a.parts, kNoIndex); }
             }
             wait_stores();
             if (lane == 0) {
@@ -368,6 +375,18 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
         if (!s_last || wave) return;
         // the last to arrive joins the parts in their order, whoever it is
         const size_t first = (size_t)r * a.parts;
+        const int total = a.parts * a.top;
+        const float *values = a.list_value + first * a.top;
+        const int *tokens = a.list_token + first * a.top;
+        constexpr int kHeld = TOP ? 6 : 0;                     // candidates that a lane asks for at once
+        float held_v[kHeld + 1];
+        int held_t[kHeld + 1];
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            const bool in = j * 64 + lane < total;
+            held_v[j] = in ? ld_coherent(values + j * 64 + lane) : -INFINITY;
+            held_t[j] = in ? ld_coherent(tokens + j * 64 + lane) : kNoIndex;
+        }
         run.init();
         for (int p = lane; p < a.parts; p += 64) {
             const LpPartial *q = a.stats + first + p;
@@ -376,23 +395,25 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
             run.add(o);
         }
         if constexpr (TOP) {
-            const int total = a.parts * a.top;
-            const float *values = a.list_value + first * a.top;
-            const int *tokens = a.list_token + first * a.top;
-            float most = -INFINITY;
-            for (int i = lane; i < total; i += 64) most = fmaxf(most, ld_coherent(values + i));
-            const float bound = lp_kth<sizeof(T) == 2>(most, a.top);
-            s_c.count = 0;
-            __builtin_amdgcn_wave_barrier();
-            for (int i = 0; i < total; i += 64) {
+            float most = -INFINITY, most_too = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) (j & 1 ? most_too : most) = fmaxf(j & 1 ? most_too : most, held_v[j]);
+            for (int i = kHeld * 64 + lane; i < total; i += 64) most = fmaxf(most, ld_coherent(values + i));
+            const float bound = lp_kth<sizeof(T) == 2>(most, most_too, a.top);
+            int n = 0;
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) lp_collect(s_c[0], n, held_v[j], held_t[j], held_v[j] >= bound && held_v[j] > -INFINITY, lane);
+            for (int i = kHeld * 64; i < total; i += 64) {
                 const bool in = i + lane < total;
                 const float v = in ? ld_coherent(values + i + lane) : -INFINITY;
-                lp_collect(s_c, v, in ? ld_coherent(tokens + i + lane) : 0, v >= bound && v > -INFINITY, lane);
+                lp_collect(s_c[0], n, v, in ? ld_coherent(tokens + i + lane) : 0, v >= bound && v > -INFINITY, lane);
             }
-            __builtin_amdgcn_wave_barrier();
-            const int n = s_c.count;
-            if (n <= 64) place = lp_place(s_c, n, lane, top_v, top_t);
-            else {
+            __builtin_amdgcn_wave_barrier();                   // LDS serves a wave's accesses in order: what its lanes wrote is there for all of them
+            if (n <= 64) {
+                if (lane < n) { top_v = s_c[0].v[lane]; top_t = s_c[0].t[lane]; }
+                else { top_v = -INFINITY; top_t = kNoIndex; }
+                place = lp_place(top_v, top_t, n, lane);
+            } else {
                 list.init();
                 for (int i = 0; i < total; i += 64) {
                     const bool in = i + lane < total;

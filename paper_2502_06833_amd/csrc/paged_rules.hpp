@@ -150,10 +150,14 @@ inline EvictPlan evict_plan(int batch, int n_kv, int held, int vec_bytes, int cu
 // ---- log probabilities ----
 // Workgroups of four waves that a row of logits goes to, and sets of `set` vectors to each (a row that does not start on a 16-byte boundary has up to one vector more)
 struct LogprobPlan { int parts, part_sets; };
+#ifndef LPT
+#define LPT 4l
+#endif
+constexpr long kLogprobTarget = LPT;
 constexpr int kLogprobTickets = 1024;      // rows that may be cut: with more there is a workgroup for every compute unit anyway
 inline LogprobPlan logprob_plan(long rows, int vocab, int set, int cus) {
     const long sets = ((vocab + 14) / 8 + set - 1) / set, most = (sets + 3) / 4;
-    const long want = rows > kLogprobTickets ? 1 : std::max(1l, std::min(most, 4l * cus / std::max(1l, rows)));
+    const long want = rows > kLogprobTickets ? 1 : std::max(1l, std::min(most, kLogprobTarget * cus / std::max(1l, rows)));
     LogprobPlan p;
     p.part_sets = (int)((sets + 4 * want - 1) / (4 * want)) * 4;
     p.parts = (int)((sets + p.part_sets - 1) / p.part_sets);
