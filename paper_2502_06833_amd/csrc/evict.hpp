@@ -14,6 +14,7 @@ struct PagedEvict {
     int keep, sinks, recent;
     int cached;                     // scores that the workgroup's LDS holds
     int columns, column_bytes;      // k_evict_move: pieces of a vector, each a workgroup's
+    int steps, shares;              // what it does, and the workgroups that share the free places
 };
 
 // Order of scores as whole numbers, the largest largest: -0 as 0, NaN below everything
@@ -24,6 +25,9 @@ __device__ __forceinline__ uint32_t evict_rank(float f) {
 }
 
 constexpr int kEvictThreads = 1024, kEvictBins = 2048;
+constexpr int kEvictAhead = 4;               // scores, or vectors, that a lane has on their way
+
+constexpr uint32_t kEvictNothing = 0x80000000u;      // the rank of 0: holes
 
 // Sum of `mine` over the waves before this one, and over all (s: 17 ints of LDS).  Called by the whole workgroup with the same value in all lanes of a wave.
 __device__ __forceinline__ int2 evict_before(int mine, int *s) {
@@ -59,9 +63,20 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_choose(PagedEvict c) {
     const int mask = (1 << c.a.page_shift) - 1;
     auto load = [&](int i) {
         const int page = paged_page(c.a, s, i);
-        return page < 0 ? 0u : evict_rank(c.scores[paged_vec(c.a, page, h, i & mask)]);
+        return page < 0 ? kEvictNothing : evict_rank(c.scores[paged_vec(c.a, page, h, i & mask)]);
     };
-    for (int i = tid; i < min(middle, c.cached); i += threads) lds[i] = load(i);
+    const int here = min(middle, c.cached);
+    for (int i0 = tid; i0 < here; i0 += threads * kEvictAhead) {
+        int page[kEvictAhead];
+        float f[kEvictAhead];
+#pragma unroll
+        for (int e = 0; e < kEvictAhead; ++e) page[e] = paged_page(c.a, s, min(i0 + e * threads, here - 1));
+#pragma unroll
+        for (int e = 0; e < kEvictAhead; ++e) f[e] = c.scores[paged_vec(c.a, max(page[e], 0), h, min(i0 + e * threads, here - 1) & mask)];
+#pragma unroll
+        for (int e = 0; e < kEvictAhead; ++e)
+            if (i0 + e * threads < here) lds[i0 + e * threads] = page[e] < 0 ? kEvictNothing : evict_rank(f[e]);
+    }
     __syncthreads();
     auto rank = [&](int i) { return i < c.cached ? lds[i] : load(i); };
     // ---- the threshold: the (cut - sinks)-th largest
@@ -78,25 +93,22 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_choose(PagedEvict c) {
                 if (pass == 0 || r >> shift == prefix) atomicAdd(&bins[(r >> low) & ((1u << bits) - 1)], 1);
             }
             __syncthreads();
-            // wave 0 goes through the bins from the top, 64 at a time
-            if (wave == 0) {
-                int above = 0;
-                for (int top = (1 << bits) - 64; top >= 0; top -= 64) {
-                    const int mine = bins[top + 63 - lane];
-                    int sum = mine;
+            // every thread adds up some bins, the largest first; the one within whose bins the count is reached says which it is
+            const int own = (1 << bits) / threads, top = (1 << bits) - 1 - tid * own;
+            int sum = 0;
+            for (int e = 0; e < own; ++e) sum += bins[top - e];
+            int upto = sum;
 #pragma unroll
-                    for (int o = 1; o < 64; o <<= 1) {
-                        const int t = __shfl_up(sum, o, kWave);
-                        sum += lane >= o ? t : 0;
-                    }
-                    const uint64_t hit = __ballot(above + sum >= need);
-                    if (hit) {
-                        const int l = __builtin_ctzll(hit);
-                        if (lane == l) { found[0] = top + 63 - l; found[1] = need - (above + sum - mine); }
-                        break;
-                    }
-                    above += __shfl(sum, 63, kWave);
-                }
+            for (int o = 1; o < 64; o <<= 1) {
+                const int t = __shfl_up(upto, o, kWave);
+                upto += lane >= o ? t : 0;
+            }
+            upto += evict_before(__builtin_amdgcn_readlane(upto, 63), part).x;
+            if (upto >= need && upto - sum < need) {
+                int left = need - (upto - sum), e = 0;
+                while (bins[top - e] < left) left -= bins[top - e++];
+                found[0] = top - e;
+                found[1] = left;
             }
             __syncthreads();
             prefix = prefix << bits | (uint32_t)found[0];
@@ -139,59 +151,67 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_choose(PagedEvict c) {
     if (tid == 0) c.counts[unit] = count;
 }
 
-// A vector's piece from one position to another; holes give zeros and take nothing.
-struct EvictPool {
-    char *base;
-    int vec_bytes, at, bytes;       // of a vector; where the piece starts, how long it is
-};
-// One workgroup moves one piece of all vectors of a (sequence, KV head): pieces do not touch each other, so the order within one is all that matters.  First the
-// free places are filled, from positions past the cut that nothing is written to meanwhile; then the last positions move down in ascending order, a block of them
-// read before it is written.
+// One workgroup moves one piece of the vectors of a (sequence, KV head); pieces do not touch each other, so the order within one is all that matters.  First the free
+// places are filled, from positions past the cut that nothing is written to meanwhile; then the last positions move down in ascending order, a block of them read before
+// it is written.  Where there may be many free places several workgroups share them, in a launch of their own (kEvictFill, then kEvictShift).  Holes give zeros and take
+// nothing.
+enum { kEvictFill = 1, kEvictShift = 2 };
 template <typename T>
-__device__ __forceinline__ void evict_piece(const PagedEvict &c, const PagedSeq &s, int h, size_t unit, char *pool, int vec_bytes, int at, int lanes) {
-    constexpr int kSteps = 4;
+__device__ __forceinline__ void evict_piece(const PagedEvict &c, const PagedSeq &s, int h, size_t unit, int share, char *pool, int vec_bytes, int at, int lanes) {
     const int mask = (1 << c.a.page_shift) - 1, per = (int)blockDim.x / lanes, lane = (int)threadIdx.x % lanes, first = (int)threadIdx.x / lanes;
-    auto place = [&](int pos) -> T * {
-        const int page = paged_page(c.a, s, pos);
-        return page < 0 ? nullptr : (T *)(pool + paged_vec(c.a, page, h, pos & mask) * vec_bytes + at) + lane;
-    };
-    const int cut = c.keep - c.recent, count = c.counts[unit];
-    const int2 *moves = c.moves + unit * (size_t)max(cut - c.sinks, 0);
-    for (int i = first; i < count; i += per) {
-        const int2 m = moves[i];
-        T *to = place(m.x);
-        const T *from = place(m.y);
-        if (to) *to = from ? *from : T{};
-    }
-    const int down = s.kv - c.keep;
-    for (int i0 = cut; i0 < c.keep; i0 += per * kSteps) {
-        T v[kSteps];
+    auto place = [&](int page, int pos) { return (T *)(pool + paged_vec(c.a, max(page, 0), h, pos & mask) * vec_bytes + at) + lane; };
+    const int cut = c.keep - c.recent;
+    if (c.steps & kEvictFill) {
+        const int count = c.counts[unit];
+        const int2 *moves = c.moves + unit * (size_t)max(cut - c.sinks, 0);
+        for (int i0 = share * per * kEvictAhead; i0 < count; i0 += c.shares * per * kEvictAhead) {
+            int2 m[kEvictAhead];
+            int from[kEvictAhead], to[kEvictAhead];
+            T v[kEvictAhead];
 #pragma unroll
-        for (int e = 0; e < kSteps; ++e) {
-            const int i = i0 + e * per + first;
-            const T *from = i < c.keep ? place(i + down) : nullptr;
-            v[e] = from ? *from : T{};
+            for (int e = 0; e < kEvictAhead; ++e) m[e] = moves[min(i0 + e * per + first, count - 1)];
+#pragma unroll
+            for (int e = 0; e < kEvictAhead; ++e) { from[e] = paged_page(c.a, s, m[e].y); to[e] = paged_page(c.a, s, m[e].x); }
+#pragma unroll
+            for (int e = 0; e < kEvictAhead; ++e) v[e] = *place(from[e], m[e].y);
+#pragma unroll
+            for (int e = 0; e < kEvictAhead; ++e)
+                if (i0 + e * per + first < count && to[e] >= 0) *place(to[e], m[e].x) = from[e] >= 0 ? v[e] : T{};
         }
+    }
+    if (!(c.steps & kEvictShift)) return;
+    const int down = s.kv - c.keep;
+    for (int i0 = cut; i0 < c.keep; i0 += per * kEvictAhead) {
+        int from[kEvictAhead], to[kEvictAhead];
+        T v[kEvictAhead];
+#pragma unroll
+        for (int e = 0; e < kEvictAhead; ++e) {
+            const int i = min(i0 + e * per + first, c.keep - 1);
+            from[e] = paged_page(c.a, s, i + down);
+            to[e] = paged_page(c.a, s, i);
+        }
+#pragma unroll
+        for (int e = 0; e < kEvictAhead; ++e) v[e] = *place(from[e], min(i0 + e * per + first, c.keep - 1) + down);
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < kSteps; ++e) {
+        for (int e = 0; e < kEvictAhead; ++e) {
             const int i = i0 + e * per + first;
-            T *to = i < c.keep ? place(i) : nullptr;
-            if (to) *to = v[e];
+            if (i < c.keep && to[e] >= 0) *place(to[e], i) = from[e] >= 0 ? v[e] : T{};
         }
     }
 }
 
 __global__ __launch_bounds__(256) void k_evict_move(PagedEvict c) {
-    const int h = (int)blockIdx.x, b = (int)blockIdx.z, part = (int)blockIdx.y;        // part: pieces of K, of V, then exponents of K and V, weights
+    // part: pieces of K, of V, then exponents of K and V, weights
+    const int h = (int)blockIdx.x % c.a.n_kv, share = (int)blockIdx.x / c.a.n_kv, part = (int)blockIdx.y, b = (int)blockIdx.z;
     const PagedSeq s = paged_seq(c.a, b);
     if (s.kv <= c.keep) return;
     const size_t unit = (size_t)b * c.a.n_kv + h;
     if (part < 2 * c.columns) {
         char *pool = (char *)(part < c.columns ? c.a.k : c.a.v);
-        evict_piece<u32x4_t>(c, s, h, unit, pool, c.columns * c.column_bytes, (part % c.columns) * c.column_bytes, c.column_bytes / 16);
-    } else if (c.a.ks && part < 2 * c.columns + 2) evict_piece<uint8_t>(c, s, h, unit, (char *)(part == 2 * c.columns ? c.a.ks : c.a.vs), 1, 0, 1);
-    else evict_piece<float>(c, s, h, unit, (char *)c.weights, 4, 0, 1);
+        evict_piece<u32x4_t>(c, s, h, unit, share, pool, c.columns * c.column_bytes, (part % c.columns) * c.column_bytes, c.column_bytes / 16);
+    } else if (c.a.ks && part < 2 * c.columns + 2) evict_piece<uint8_t>(c, s, h, unit, share, (char *)(part == 2 * c.columns ? c.a.ks : c.a.vs), 1, 0, 1);
+    else evict_piece<float>(c, s, h, unit, share, (char *)c.weights, 4, 0, 1);
 }
 
 }  // namespace ead

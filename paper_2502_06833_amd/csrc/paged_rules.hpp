@@ -133,17 +133,21 @@ inline WeighPlan weigh_many(int batch, int n_kv, long rows, int held, int cus) {
 }
 
 // ---- eviction ----
-constexpr int kEvictCached = 12288;        // scores of a sequence and head that a workgroup keeps in LDS
+constexpr int kEvictCached = 32768;        // scores of a sequence and head that a workgroup keeps in LDS at most
+constexpr int kEvictPlainCached = 12288;   // those that it gets without asking for more LDS than 64 KB
 inline unsigned long long evict_moves_at(unsigned long long units) { return (units * 4 + 15) / 16 * 16; }
 struct EvictPlan {
     int threads;                           // of a workgroup that chooses
     int columns;                           // pieces of a vector that workgroups of their own move
+    int shares;                            // workgroups that share a sequence's and head's free places: more than one has a launch of its own
 };
-inline EvictPlan evict_plan(int batch, int n_kv, int held, int vec_bytes, int cus) {
+inline EvictPlan evict_plan(int batch, int n_kv, int held, int keep, int recent, int vec_bytes, int cus) {
     EvictPlan p;
+    const long units = (long)batch * n_kv, moves = std::max(0, std::min(held - keep, keep - recent));
     p.threads = held > 4096 ? 1024 : 256;
     p.columns = 1;
-    while (vec_bytes / p.columns > 64 && 2l * batch * n_kv * p.columns < 2l * cus) p.columns *= 2;
+    while (vec_bytes / p.columns > 64 && 2 * units * p.columns < 2l * cus) p.columns *= 2;
+    p.shares = moves > 512 ? (int)std::max(1l, std::min(moves / 256, 8l * cus / (2 * units * p.columns))) : 1;
     return p;
 }
 

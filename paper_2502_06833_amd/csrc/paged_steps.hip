@@ -1,6 +1,8 @@
 // Host side of the steps around a paged cache's attention: ead_rotate, ead_paged_append, ead_paged_weigh, ead_paged_evict.
 #include <math.h>
 
+#include <atomic>
+
 #include "evict.hpp"
 #include "paged_host.hpp"
 #include "paged_rules.hpp"
@@ -53,6 +55,24 @@ ead_status check_weigh(const ead_paged_cache *cache, const ead_paged_batch *batc
 }
 
 int held_of(const ead_paged_cache *c, const ead_paged_batch *b) { return (int)std::min((long)b->max_kv, (long)b->table_width * c->page_size); }
+
+// Scores that k_evict_choose may keep in LDS on the current device
+int evict_room() {
+    constexpr int kDevices = 64;
+    static std::atomic<int> room[kDevices];              // 0: not asked yet
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kDevices) return kEvictPlainCached;
+    int n = room[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        n = kEvictCached;
+        if (hipFuncSetAttribute((const void *)k_evict_choose, hipFuncAttributeMaxDynamicSharedMemorySize, kEvictCached * 4) != hipSuccess) {
+            (void)hipGetLastError();
+            n = kEvictPlainCached;
+        }
+        room[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
 
 // How a call of ead_paged_weigh is cut: the workspace is the same whatever the queries' alignment lets it do
 struct WeighCall {
@@ -230,14 +250,21 @@ ead_status ead_paged_evict(const ead_paged_cache *cache, const ead_paged_batch *
     c.moves = (int2 *)((char *)workspace + evict_moves_at((uint64_t)batch->batch * cache->n_kv_heads));
     c.keep = ev->keep; c.sinks = ev->sinks; c.recent = ev->recent;
     const int held = held_of(cache, batch), vec_bytes = cache->head_dim * element_bytes(cache->dtype);
-    c.cached = std::min(held, kEvictCached);
-    const EvictPlan p = evict_plan(batch->batch, cache->n_kv_heads, held, vec_bytes, compute_units());
+    c.cached = std::min(held, evict_room());
+    const EvictPlan p = evict_plan(batch->batch, cache->n_kv_heads, held, ev->keep, ev->recent, vec_bytes, compute_units());
     c.columns = p.columns; c.column_bytes = vec_bytes / p.columns;
     hipLaunchKernelGGL(k_evict_choose, dim3((unsigned)cache->n_kv_heads, (unsigned)batch->batch), dim3(p.threads), (size_t)c.cached * 4, (hipStream_t)hip_stream, c);
-    PAGED_TRY(launched("ead_paged_evict"));
-    const unsigned parts = 2 * p.columns + (cache->dtype == EAD_FP8 ? 2 : 0) + (weights ? 1 : 0);         // the weights are the last
-    if ((long)batch->table_width * cache->page_size > ev->keep)
-        hipLaunchKernelGGL(k_evict_move, dim3((unsigned)cache->n_kv_heads, parts, (unsigned)batch->batch), dim3(256), 0, (hipStream_t)hip_stream, c);
+    if ((long)batch->table_width * cache->page_size > ev->keep) {
+        const unsigned parts = 2 * p.columns + (cache->dtype == EAD_FP8 ? 2 : 0) + (weights ? 1 : 0);         // the weights are the last
+        auto move = [&](int steps, int shares) {
+            c.steps = steps; c.shares = shares;
+            hipLaunchKernelGGL(k_evict_move, dim3((unsigned)(cache->n_kv_heads * shares), parts, (unsigned)batch->batch), dim3(256), 0, (hipStream_t)hip_stream, c);
+        };
+        if (p.shares > 1) {
+            move(kEvictFill, p.shares);
+            if (ev->recent) move(kEvictShift, 1);
+        } else move(kEvictFill | kEvictShift, 1);
+    }
     return launched("ead_paged_evict");
 }
 
