@@ -399,7 +399,8 @@ ead_status ead_paged_weigh(const ead_paged_cache *cache, const ead_paged_batch *
  * keep - recent, in their order.  K, V, their scales and `weights` (null: none; may be the scores) move; kept[b][h][i] is the position that now lies at
  * i, -1 from the sequence's length on.  kv_lens is not changed, since other layers' caches still need it: afterwards the
  * sequence holds min(kv_len, keep) positions.  q_starts, rows and max_q are not looked at.  Holes have the score 0; what is moved
- * from one is zeros, what is moved to one is lost.  The sequences' pages are theirs alone. */
+ * from one is zeros, what is moved to one is lost.  The sequences' pages are theirs alone.  `scores` is 16-byte aligned, max_kv at
+ * most 2^20; a sequence that holds more than max_kv is left as it is, with -1 in kept. */
 typedef struct { int32_t keep, sinks, recent; } ead_paged_eviction;
 /* Bytes of device memory the call needs, 16-byte aligned; nothing has to clear them, and no two calls at once share them. */
 ead_status ead_paged_evict_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_eviction *eviction,

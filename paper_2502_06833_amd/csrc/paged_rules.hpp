@@ -133,13 +133,17 @@ inline WeighPlan weigh_many(int batch, int n_kv, long rows, int held, int cus) {
 }
 
 // ---- eviction ----
-constexpr int kEvictCached = 32768;        // scores of a sequence and head that a workgroup keeps in LDS at most
-constexpr int kEvictPlainCached = 12288;   // those that it gets without asking for more LDS than 64 KB
+constexpr int kEvictMost = 1 << 20;        // positions of a sequence at most
+// LDS of a workgroup that chooses: a bit for every position that the host vouched for, and as many scores' ranks as there is room for
+constexpr int kEvictLds = 144 << 10, kEvictPlainLds = 52 << 10;      // all that a compute unit has beside the bins; what needs no asking for
+inline int evict_words(int held) { return (held + 63) / 64; }
+inline int evict_cached(int held, int room) { return std::min((std::max(held, 1) + 3) / 4 * 4, (room - evict_words(held) * 8) / 16 * 4); }
 inline unsigned long long evict_moves_at(unsigned long long units) { return (units * 4 + 15) / 16 * 16; }
 struct EvictPlan {
     int threads;                           // of a workgroup that chooses
     int columns;                           // pieces of a vector that workgroups of their own move
-    int shares;                            // workgroups that share a sequence's and head's free places: more than one has a launch of its own
+    int shares;                            // workgroups that share a sequence's and head's free places (whole vectors, in a launch of their own); 0: the same ones
+    int shift_threads;                     // of a workgroup that moves the last positions down
 };
 inline EvictPlan evict_plan(int batch, int n_kv, int held, int keep, int recent, int vec_bytes, int cus) {
     EvictPlan p;
@@ -147,7 +151,8 @@ inline EvictPlan evict_plan(int batch, int n_kv, int held, int keep, int recent,
     p.threads = held > 4096 ? 1024 : 256;
     p.columns = 1;
     while (vec_bytes / p.columns > 64 && 2 * units * p.columns < 2l * cus) p.columns *= 2;
-    p.shares = moves > 512 ? (int)std::max(1l, std::min(moves / 256, 8l * cus / (2 * units * p.columns))) : 1;
+    p.shares = moves > 512 ? (int)std::max(1l, std::min(moves / 64, 8l * cus / (2 * units))) : 0;
+    p.shift_threads = 2 * units * p.columns <= 2l * cus ? 1024 : 256;
     return p;
 }
 

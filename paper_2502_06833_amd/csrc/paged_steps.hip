@@ -56,18 +56,18 @@ ead_status check_weigh(const ead_paged_cache *cache, const ead_paged_batch *batc
 
 int held_of(const ead_paged_cache *c, const ead_paged_batch *b) { return (int)std::min((long)b->max_kv, (long)b->table_width * c->page_size); }
 
-// Scores that k_evict_choose may keep in LDS on the current device
+// LDS that k_evict_choose may use on the current device beside its own arrays
 int evict_room() {
     constexpr int kDevices = 64;
     static std::atomic<int> room[kDevices];              // 0: not asked yet
     int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kDevices) return kEvictPlainCached;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kDevices) return kEvictPlainLds;
     int n = room[dev].load(std::memory_order_relaxed);
     if (n == 0) {
-        n = kEvictCached;
-        if (hipFuncSetAttribute((const void *)k_evict_choose, hipFuncAttributeMaxDynamicSharedMemorySize, kEvictCached * 4) != hipSuccess) {
+        n = kEvictLds;
+        if (hipFuncSetAttribute((const void *)k_evict_choose, hipFuncAttributeMaxDynamicSharedMemorySize, kEvictLds) != hipSuccess) {
             (void)hipGetLastError();
-            n = kEvictPlainCached;
+            n = kEvictPlainLds;
         }
         room[dev].store(n, std::memory_order_relaxed);
     }
@@ -230,6 +230,7 @@ ead_status ead_paged_evict_workspace(const ead_paged_cache *cache, const ead_pag
     if (!ev) return refuse(EAD_ERR_INVALID_ARG, "eviction is null");
     if (ev->keep < 1 || ev->sinks < 0 || ev->recent < 0 || (long)ev->sinks + ev->recent > ev->keep)
         return refuse(EAD_ERR_INVALID_ARG, "eviction: need keep >= 1, sinks >= 0, recent >= 0 and sinks + recent <= keep");
+    if (held_of(cache, batch) > kEvictMost) return refuse(EAD_ERR_SHAPE, "batch: sequences of up to 2^20 positions can be cut, max_kv is %d", batch->max_kv);
     const uint64_t units = (uint64_t)batch->batch * cache->n_kv_heads;
     *bytes = evict_moves_at(units) + units * (uint64_t)(ev->keep - ev->sinks - ev->recent) * 8;
     return EAD_OK;
@@ -240,7 +241,8 @@ ead_status ead_paged_evict(const ead_paged_cache *cache, const ead_paged_batch *
     uint64_t need = 0;
     PAGED_TRY(ead_paged_evict_workspace(cache, batch, ev, &need));
     if (!scores || !kept) return refuse(EAD_ERR_INVALID_ARG, "scores or kept is null");
-    if (((uintptr_t)scores | (uintptr_t)weights | (uintptr_t)kept) & 3) return refuse(EAD_ERR_INVALID_ARG, "scores, weights or kept is not aligned to its elements");
+    if ((uintptr_t)scores & 15) return refuse(EAD_ERR_INVALID_ARG, "scores have to be 16-byte aligned");
+    if (((uintptr_t)weights | (uintptr_t)kept) & 3) return refuse(EAD_ERR_INVALID_ARG, "weights or kept is not aligned to its elements");
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))
         return refuse(EAD_ERR_INVALID_ARG, "workspace: %llu bytes, 16-byte aligned, are needed", (unsigned long long)need);
     PagedEvict c{};
@@ -250,20 +252,23 @@ ead_status ead_paged_evict(const ead_paged_cache *cache, const ead_paged_batch *
     c.moves = (int2 *)((char *)workspace + evict_moves_at((uint64_t)batch->batch * cache->n_kv_heads));
     c.keep = ev->keep; c.sinks = ev->sinks; c.recent = ev->recent;
     const int held = held_of(cache, batch), vec_bytes = cache->head_dim * element_bytes(cache->dtype);
-    c.cached = std::min(held, evict_room());
+    c.held = held;
+    c.cached = evict_cached(held, evict_room());
+    if (c.cached < 4) return refuse(EAD_ERR_SHAPE, "batch: max_kv %d is more than this device's local memory lets be cut", held);
     const EvictPlan p = evict_plan(batch->batch, cache->n_kv_heads, held, ev->keep, ev->recent, vec_bytes, compute_units());
-    c.columns = p.columns; c.column_bytes = vec_bytes / p.columns;
-    hipLaunchKernelGGL(k_evict_choose, dim3((unsigned)cache->n_kv_heads, (unsigned)batch->batch), dim3(p.threads), (size_t)c.cached * 4, (hipStream_t)hip_stream, c);
-    if ((long)batch->table_width * cache->page_size > ev->keep) {
-        const unsigned parts = 2 * p.columns + (cache->dtype == EAD_FP8 ? 2 : 0) + (weights ? 1 : 0);         // the weights are the last
-        auto move = [&](int steps, int shares) {
+    const size_t lds = (size_t)c.cached * 4 + (size_t)evict_words(held) * 8;
+    hipLaunchKernelGGL(k_evict_choose, dim3((unsigned)cache->n_kv_heads, (unsigned)batch->batch), dim3(p.threads), lds, (hipStream_t)hip_stream, c);
+    if (held > ev->keep) {
+        auto move = [&](int steps, int columns, int shares, int threads) {
             c.steps = steps; c.shares = shares;
-            hipLaunchKernelGGL(k_evict_move, dim3((unsigned)(cache->n_kv_heads * shares), parts, (unsigned)batch->batch), dim3(256), 0, (hipStream_t)hip_stream, c);
+            c.columns = columns; c.column_bytes = vec_bytes / columns;
+            const unsigned parts = 2 * columns + (cache->dtype == EAD_FP8 ? 2 : 0) + (weights ? 1 : 0);       // the weights are the last
+            hipLaunchKernelGGL(k_evict_move, dim3((unsigned)(cache->n_kv_heads * shares), parts, (unsigned)batch->batch), dim3(threads), 0, (hipStream_t)hip_stream, c);
         };
-        if (p.shares > 1) {
-            move(kEvictFill, p.shares);
-            if (ev->recent) move(kEvictShift, 1);
-        } else move(kEvictFill | kEvictShift, 1);
+        if (p.shares) {
+            move(kEvictFill, 1, p.shares, 256);
+            if (ev->recent) move(kEvictShift, p.columns, 1, p.shift_threads);
+        } else move(kEvictFill | kEvictShift, p.columns, 1, p.shift_threads);
     }
     return launched("ead_paged_evict");
 }
