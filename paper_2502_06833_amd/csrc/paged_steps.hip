@@ -87,7 +87,7 @@ WeighCall weigh_of(const ead_paged_cache *c, const ead_paged_batch *b, const ead
     WeighCall w{};
     w.few = rows <= weigh_few_rows(c->dtype == EAD_F32, c->head_dim);
     w.blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    w.tiles = weigh_tiles((long)b->batch * c->n_kv_heads, held, kWeighTiles, compute_units());
+    w.tiles = weigh_tiles((long)b->batch * c->n_kv_heads, held, compute_units());
     if (!w.few && c->dtype != EAD_F32) {
         w.m = weigh_many(b->batch, c->n_kv_heads, rows, held, compute_units());
         if (w.m.splits > 1) w.bytes = (uint64_t)w.m.splits * b->batch * c->n_kv_heads * w.m.part_keys * 4;

@@ -4,6 +4,8 @@
 
 namespace ead {
 
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
 struct PagedWeigh {
     PagedArgs a;
     RowsArg q;
@@ -12,7 +14,7 @@ struct PagedWeigh {
     int n_heads, group;             // group: query heads per KV head
     float c2;                       // scale * log2(e)
     int window, sinks;
-    int tiles;                      // k_weigh_few: tiles of 32 keys to a wave
+    int tiles;                      // k_weigh_few: tiles of 32 keys to a wave, 32 at most (their pages lie in its lanes)
     int splits, part_keys;          // k_weigh_many: ranges of rows; keys of a range's sums
     float *part;                    // [range][sequence][KV head][key]
 };
@@ -108,16 +110,19 @@ struct WeighWave {
     static constexpr int kReq = 16 * kRow / 1024 > 0 ? 16 * kRow / 1024 : 1;  // requests for 16 keys (8-bit HD 32: for 32)
     static constexpr bool kShort = 16 * kRow < 1024;
     static constexpr int kTile = kKeys + 256 + (F8 ? 256 : 0), kRequests = (kShort ? 1 : 2 * kReq) + 1 + (F8 ? 1 : 0);
-    static constexpr int kRing = kKeys >= 8192 ? 2 : 16384 / kKeys;           // tiles
+    static constexpr int kRing = kKeys >= 4096 ? 2 : 8192 / kKeys;             // tiles
     static constexpr int KE = F32 ? 4 : F8 ? (HD >= 64 ? 16 : 8) : 8;         // neighbouring elements of K in one read
     static constexpr int KL = HD / 4 / KE;                                    // reads per key
     static constexpr int QW = F32 ? HD / 4 : HD / 8;                          // words of Q per lane
+    static constexpr int kBlocks = 4 * kRing * kTile <= 40960 && NB < 4 ? 4 : 2;   // workgroups to a compute unit
 };
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-constexpr int kWeighTiles = 32;      // tiles of 32 keys that a wave takes at most: their pages lie in its lanes
+// 4 bytes per lane from base + voff (base the same in all lanes) to LDS at lds + 4 lane
+__device__ __forceinline__ void request_words_from(const void *base, uint32_t voff, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(voff), "s"(base) : "memory");
+}
 
 template <typename CT, int HD, int NB>
-__global__ __launch_bounds__(256, 2) void k_weigh_few(PagedWeigh c) {
+__global__ __launch_bounds__(256, (WeighWave<CT, HD, NB>::kBlocks)) void k_weigh_few(PagedWeigh c) {
     using W = WeighWave<CT, HD, NB>;
     constexpr int kRow = W::kRow;
     __shared__ __align__(1024) char lds[4 * W::kRing * W::kTile];
@@ -136,14 +141,16 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(PagedWeigh c) {
     }
     // element KE (4 i + g) + .. of a row's queries belongs to K's read i: the contraction's order is free as long as both have the same
     uint32_t q[NB][W::QW];
-    float nl[NB][4];                                         // -lse in bits of this lane's rows, -inf where there is none
-    int p_lo = s.first, p_hi = s.first + (rows - 1) / c.group;
+    float nl[NB][4];                                         // -lse in bits of this lane's rows, far below anything where one pays nothing or there is none
+    const int p_lo = s.first, p_hi = s.first + (rows - 1) / c.group;
+    bool odd = false;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
         for (int i = 0; i < W::QW; ++i) q[b][i] = 0u;
-        const int r = b * 16 + n, tok = r / c.group, qh = h * c.group + r % c.group;
-        if (r < rows) {
+        // (past the last row: that one again, which adds nothing that it does not)
+        const int r = min(b * 16 + n, rows - 1), tok = r / c.group, qh = h * c.group + r % c.group;
+        {
             const size_t at = (size_t)(s.row0 + tok) * c.q.row_stride + (size_t)qh * c.q.head_stride;
 #pragma unroll
             for (int i = 0; i < W::KL; ++i) {
@@ -164,9 +171,11 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(PagedWeigh c) {
             const int rr = b * 16 + 4 * g + e;
             float z = -INFINITY;
             if (rr < rows) z = c.lse[(size_t)(s.row0 + rr / c.group) * c.n_heads + h * c.group + rr % c.group];
-            nl[b][e] = z == -INFINITY ? -INFINITY : -1.4426950408889634f * z;
+            odd |= rr < rows && z == -INFINITY;
+            nl[b][e] = z == -INFINITY ? -1e30f : -1.4426950408889634f * z;
         }
     }
+    odd = __any(odd);
     uint32_t from[W::kReq], k_at[W::KL];
 #pragma unroll
     for (int e = 0; e < W::kReq; ++e) {                      // where this lane's piece of a request lies among 16 keys
@@ -193,8 +202,14 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(PagedWeigh c) {
 #pragma unroll
             for (int e = 0; e < W::kReq; ++e) request_tile<true>((const bf16_t *)((const char *)c.a.k + vec1 * kRow), from[e], to + (W::kReq + e) * 1024);
         }
-        request_words(c.weights + (lane & 16 ? vec1 : vec0) + (lane & 15), to + W::kKeys);        // lanes 0 .. 31: the tile's keys; the others repeat them
-        if constexpr (W::F8) request_words(c.a.ks + (lane & 4 ? vec1 : vec0) + 4 * (lane & 3), to + W::kKeys + 256);
+        // weights, in lanes 0 .. 31, and exponents, four to a word, in lanes 0 .. 7; the others repeat them
+        if (vec1 == vec0 + 16) {
+            request_words_from(c.weights + vec0, 4 * (lane & 31), to + W::kKeys);
+            if constexpr (W::F8) request_words_from(c.a.ks + vec0, 4 * (lane & 7), to + W::kKeys + 256);
+        } else {
+            request_words(c.weights + (lane & 16 ? vec1 : vec0) + n, to + W::kKeys);
+            if constexpr (W::F8) request_words(c.a.ks + (lane & 4 ? vec1 : vec0) + 4 * (lane & 3), to + W::kKeys + 256);
+        }
     };
     auto take = [&](int i, auto edge_c) {
         constexpr bool EDGE = decltype(edge_c)::value;
@@ -245,21 +260,20 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(PagedWeigh c) {
                 for (int e = 0; e < 4; ++e) {
                     const int rr = b * 16 + 4 * g + e;
                     float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][e], c.c2, nl[b][e]));
-                    // a row that pays nothing does so to an infinite key too
-                    x = nl[b][e] == -INFINITY ? 0.f : x;
-                    if constexpr (EDGE) x = rr < rows && weigh_sees(c, s.first + rr / c.group, base + 16 * half + n) ? x : 0.f;
+                    if constexpr (EDGE) x = rr < rows && nl[b][e] != -1e30f && weigh_sees(c, s.first + rr / c.group, base + 16 * half + n) ? x : 0.f;
                     t += x;
                 }
-            t += __shfl_xor(t, 16, kWave);
-            t += __shfl_xor(t, 32, kWave);
             sum[half] = t;
         }
-        // lanes 0 .. 15 have the first half's keys, 16 .. 31 the second's
-        const int key = base + (lane & 31), page = __builtin_amdgcn_readlane(pages, 2 * i), page_too = __builtin_amdgcn_readlane(pages, 2 * i + 1);
-        const int mine = lane & 16 ? page_too : page;
-        const float old = lds_read<float>(at + W::kKeys + 4 * (lane & 31));
-        if (lane < 32 && mine >= 0 && key < s.kv)
-            c.weights[paged_vec(c.a, mine, h, key & page_mask)] = (key < s.first ? old : 0.f) + (lane & 16 ? sum[1] : sum[0]);
+        // both halves' four sums a key at once: the first half's come to lanes 0 .. 15 and 16 .. 31, the second's to the others
+        const auto over = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[0]), __float_as_uint(sum[1]), false, false);
+        const uint32_t two = __float_as_uint(__uint_as_float(over[0]) + __uint_as_float(over[1]));
+        const auto row = __builtin_amdgcn_permlane16_swap(two, two, false, false);
+        const float paid = __uint_as_float(row[0]) + __uint_as_float(row[1]);
+        const int key = base + 16 * (lane >> 5) + n, page = __builtin_amdgcn_readlane(pages, 2 * i), page_too = __builtin_amdgcn_readlane(pages, 2 * i + 1);
+        const int mine = lane & 32 ? page_too : page;
+        const float old = lds_read<float>(at + W::kKeys + 64 * (lane >> 5) + 4 * n);
+        if (!(lane & 16) && mine >= 0 && key < s.kv) c.weights[paged_vec(c.a, mine, h, key & page_mask)] = (key < s.first ? old : 0.f) + paid;
     };
 #pragma unroll
     for (int i = 0; i < W::kRing - 1; ++i)
@@ -270,7 +284,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(PagedWeigh c) {
             wait_requests<(W::kRing - 1) * W::kRequests>();
         } else wait_requests<0>();
         const int base = key0 + i * 128, last = base + 31;
-        if (last <= p_lo && (!c.window || p_hi - base < c.window || last < c.sinks)) take(i, std::false_type{});
+        if (last <= p_lo && !odd && (!c.window || p_hi - base < c.window || last < c.sinks)) take(i, std::false_type{});
         else take(i, std::true_type{});
     }
 }
@@ -318,33 +332,34 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(PagedWeigh c) {
             } else k[b][i] = __builtin_bit_cast(bf16x8_t, *(gptr<u32x4_t>)((const bf16_t *)c.a.k + vec[b] * HD + d));
         }
     }
-    // ---- staging: a request is 16 bytes to a lane; this lane's pieces of a tile belong to rows r_of[e], which advance by 32 rows a tile without a division
+    // ---- staging: a request is 16 bytes to a lane, whose address goes on by 32 rows a tile without a product
     const uint32_t base = lds_address(lds);
     constexpr int kPieces = kReq > 0 ? kReq : 1;
     const bool asks = kReq > 0 || wave < 2;
-    int tok[kPieces], rem[kPieces], piece[kPieces], row_at[kPieces];
+    int rem[kPieces], row_at[kPieces];
+    const bf16_t *from[kPieces];
+    const int step_tok = 32 / c.group, step_rem = 32 % c.group;
+    const long step = step_tok * c.q.row_stride + step_rem * c.q.head_stride, wrap = c.q.row_stride - c.group * c.q.head_stride;
+    const bf16_t *first_row = (const bf16_t *)c.q.p + (size_t)s.row0 * c.q.row_stride + (size_t)(h * c.group) * c.q.head_stride;
 #pragma unroll
     for (int e = 0; e < kPieces; ++e) {
         const int at = (kReq > 0 ? wave * kReq + e : wave & 1) * 1024 + lane * 16, r = at / kRowBytes;
-        piece[e] = ((at % kRowBytes >> 4) ^ lds_swizzle<kRowBytes>(r)) * 8;
         row_at[e] = t0 * 32 + r;
-        tok[e] = row_at[e] / c.group;
+        const int tok = row_at[e] / c.group;
         rem[e] = row_at[e] % c.group;
+        from[e] = first_row + tok * c.q.row_stride + rem[e] * c.q.head_stride + ((at % kRowBytes >> 4) ^ lds_swizzle<kRowBytes>(r)) * 8;
     }
-    const int step_tok = 32 / c.group, step_rem = 32 % c.group;
     int z_row = t0 * 32 + lane, z_tok = z_row / c.group, z_rem = z_row % c.group;          // wave 0, lanes 0 .. 31: the tile's lse
     auto request = [&](int t) {
         const uint32_t to = __builtin_amdgcn_readfirstlane(base + (t & 1) * kTileBytes + (kReq > 0 ? wave * kReq : wave & 1) * 1024);
         if (!asks) return;
 #pragma unroll
         for (int e = 0; e < kPieces; ++e) {
-            const bool in = row_at[e] < rows;                // past the last row: the first one, whose scores are left out
-            const size_t at = (size_t)(s.row0 + (in ? tok[e] : 0)) * c.q.row_stride + (size_t)(h * c.group + (in ? rem[e] : 0)) * c.q.head_stride;
-            request_pieces((const bf16_t *)c.q.p + at + piece[e], to + e * 1024);
+            request_pieces(row_at[e] < rows ? from[e] : first_row, to + e * 1024);         // past the last row: a row whose scores are left out
             row_at[e] += 32;
-            tok[e] += step_tok;
             rem[e] += step_rem;
-            if (rem[e] >= c.group) { rem[e] -= c.group; ++tok[e]; }
+            from[e] += step + (rem[e] >= c.group ? wrap : 0);
+            rem[e] -= rem[e] >= c.group ? c.group : 0;
         }
     };
     auto next_lse = [&] {

@@ -257,7 +257,7 @@ class PagedCache:
         _fits(n_pages=n)
         self._device = k_pages.get_device()
         self._key = (self._code, self.page_size, self.n_kv_heads, self.head_dim)
-        self._attention = lib().ead_paged_attention
+        self._attention, self._append, self._weigh = lib().ead_paged_attention, lib().ead_paged_append, lib().ead_paged_weigh
         self._scale = 1.0 / float(self.head_dim) ** 0.5
 
     @classmethod
@@ -338,13 +338,18 @@ class PagedCache:
         rv = _rows("v", v, self, rows, self.n_kv_heads)
         if out is None:
             out = _empty_like(q)
+            ro = Rows(out.data_ptr(), n_heads * self.head_dim, self.head_dim)
         elif out.dtype != q.dtype:
             raise ValueError(f"out: {q.dtype} is needed, got {out.dtype}")
-        ro = _outputs("out", out, self, rows, n_heads)
+        else:
+            ro = _outputs("out", out, self, rows, n_heads)
         at = None if positions is None else _positions(positions, rows, self._device)
         stream = _stream(self, batch)
         if rows:
-            _check(lib().ead_paged_append(self._ref, batch._ref, rotary._ref, code, n_heads, at, C.byref(rq), C.byref(rk), C.byref(rv), C.byref(ro), stream))
+            byref = C.byref
+            rc = self._append(self._ref, batch._ref, rotary._ref, code, n_heads, at, byref(rq), byref(rk), byref(rv), byref(ro), stream)
+            if rc:
+                _check(rc)
         return out
 
     def new_weights(self):
@@ -377,7 +382,9 @@ class PagedCache:
         args = (n_heads, F32 if self._code == F32 else BF16, window, sinks, self._scale if scale is None else scale, 0)
         d, need, _ = batch._sized("ead_paged_weigh_workspace", self, args, AttnDesc)
         ws = _scratch(lse, need)
-        _check(lib().ead_paged_weigh(self._ref, batch._ref, d, C.byref(rq), lse.data_ptr(), to, ws.data_ptr() if need else None, need, stream))
+        rc = self._weigh(self._ref, batch._ref, d, C.byref(rq), lse.data_ptr(), to, ws.data_ptr() if need else None, need, stream)
+        if rc:
+            _check(rc)
         return weights
 
     def evict(self, batch, scores, keep, sinks=0, recent=0, weights=None, kept=None):

@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 
 from .binding import lib
-from .paged import FP8, _check, _code, _current_device, _empty_like, _outputs, _positions, _rows, _stream_ptr
+from .paged import FP8, Rows, _check, _code, _current_device, _empty_like, _outputs, _positions, _rows, _stream_ptr
 
 
 class RotaryDesc(C.Structure):
@@ -55,13 +55,15 @@ class Rotary:
         ptr = [g.data_ptr() if g is not None else None for g in (q_gain, k_gain)]
         self._desc = RotaryDesc(head_dim, rotary_dim, interleaved, bool(gains) and gains[0].dim() == 2, eps, self.inv_freq.data_ptr() if rotary_dim else None, *ptr)
         self._ref = C.byref(self._desc)
+        self._rotate = lib().ead_rotate
 
     def _fits(self, head_dim, device, n_heads, n_kv_heads):
         if head_dim != self.head_dim or device != self._device:
             raise ValueError(f"vectors of {head_dim} on GPU {device}, but a Rotary for {self.head_dim} on GPU {self._device}")
-        for name, have, need in (("q_gain", self._heads[0], n_heads), ("k_gain", self._heads[1], n_kv_heads)):
-            if have is not None and have != need:
-                raise ValueError(f"{name}: gains of {have} heads, {need} are needed")
+        if self._desc.gain_per_head:
+            for name, have, need in (("q_gain", self._heads[0], n_heads), ("k_gain", self._heads[1], n_kv_heads)):
+                if have is not None and have != need:
+                    raise ValueError(f"{name}: gains of {have} heads, {need} are needed")
 
     def __call__(self, q, k, positions, out=None):
         """(q, k) [rows, heads, head_dim] of float32 or bfloat16 (any row and head strides) normalised and turned by positions, int32 [rows]: new tensors, or
@@ -76,13 +78,19 @@ class Rotary:
         rq, rk = _rows("q", q, self, rows, n_heads), _rows("k", k, self, rows, n_kv)
         if out is None:
             out = (_empty_like(q), _empty_like(k))
+            dim = self.head_dim
+            oq, ok = Rows(out[0].data_ptr(), n_heads * dim, dim), Rows(out[1].data_ptr(), n_kv * dim, dim)
         elif out[0].dtype != q.dtype or out[1].dtype != q.dtype:
             raise ValueError(f"out: {q.dtype} is needed, got {out[0].dtype} and {out[1].dtype}")
-        oq, ok = _outputs("out", out[0], self, rows, n_heads), _outputs("out", out[1], self, rows, n_kv)
+        else:
+            oq, ok = _outputs("out", out[0], self, rows, n_heads), _outputs("out", out[1], self, rows, n_kv)
         at = _positions(positions, rows, self._device)
         stream = _stream_ptr()
         if _current_device() != self._device:
             raise ValueError(f"tensors on GPU {self._device}, but GPU {_current_device()} is the current one (torch.cuda.set_device, torch.cuda.device)")
         if rows and n_heads + n_kv:
-            _check(lib().ead_rotate(self._ref, code, rows, n_heads, n_kv, at, C.byref(rq), C.byref(rk), C.byref(oq), C.byref(ok), stream))
+            byref = C.byref
+            rc = self._rotate(self._ref, code, rows, n_heads, n_kv, at, byref(rq), byref(rk), byref(oq), byref(ok), stream)
+            if rc:
+                _check(rc)
         return out

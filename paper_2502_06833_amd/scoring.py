@@ -31,22 +31,23 @@ class _Workspaces:
         self._eager, self._captured = {}, (None, {})
 
     def get(self, need, device, stream):
-        import torch
-        of, key = self._eager, (device.index, stream)
+        of, key = self._eager, (device, stream)
         if paged._capturing():
             n = C.c_uint64(0)
             _check(lib().ead_stream_capture(C.c_void_p(stream), C.byref(n)))
-            if self._captured[0] != (device.index, n.value):
-                self._captured = ((device.index, n.value), {})
+            if self._captured[0] != (device, n.value):
+                self._captured = ((device, n.value), {})
             of = self._captured[1]
         ws = of.get(key)
         if ws is None or ws.numel() * 4 < need:
-            ws = of[key] = torch.zeros((need + 3) // 4, dtype=torch.int32, device=device)
+            import torch
+            ws = of[key] = torch.zeros((need + 3) // 4, dtype=torch.int32, device=torch.device("cuda", device))
         return ws.data_ptr()
 
 
 _workspaces = _Workspaces()
 _dtypes = None
+_needs = {}                     # (rows, vocab, top): bytes
 
 
 def logprobs(logits, tokens=None, top=0, unit=NATS):
@@ -59,9 +60,11 @@ def logprobs(logits, tokens=None, top=0, unit=NATS):
     code = _dtypes.get(logits.dtype)
     if code is None:
         raise TypeError(f"unsupported dtype {logits.dtype}")
-    if not logits.is_cuda or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1) or (logits.stride(0) < 0):
-        raise ValueError("logits: [rows, vocab] on the GPU whose rows are contiguous are needed")
-    rows, vocab = logits.shape
+    if not logits.is_cuda or logits.dim() != 2:
+        raise ValueError("logits: [rows, vocab] on the GPU are needed")
+    (rows, vocab), (stride, apart) = logits.shape, logits.stride()
+    if apart != 1 and vocab > 1:
+        raise ValueError("logits: rows whose elements lie side by side are needed")
     if vocab < 1 or top < 0 or top > min(32, vocab):
         raise ValueError(f"top {top} is not in 0 .. {min(32, vocab)} (vocab {vocab})")
     device = logits.get_device()
@@ -73,9 +76,18 @@ def logprobs(logits, tokens=None, top=0, unit=NATS):
     H = logits.new_empty(rows, dtype=f32)
     lp, rank = (logits.new_empty(rows, dtype=f32), logits.new_empty(rows, dtype=i32)) if tokens is not None else (None, None)
     tt, tl = (logits.new_empty((rows, top), dtype=i32), logits.new_empty((rows, top), dtype=f32)) if top else (None, None)
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    d = CallDesc(logits.data_ptr(), code, rows, vocab, logits.stride(0) if rows > 1 else vocab, ptr(tokens), top, unit, ptr(lp), H.data_ptr(), ptr(rank), ptr(tt), ptr(tl))
-    ref, need, stream = C.byref(d), C.c_uint64(0), _stream_ptr()
-    _check(lib().ead_logprobs_workspace(ref, C.byref(need)))
-    _check(lib().ead_logprobs(ref, _workspaces.get(need.value, logits.device, stream) if need.value else None, need.value, stream))
+    given, more = tokens is not None, top > 0
+    d = CallDesc(logits.data_ptr(), code, rows, vocab, stride if rows > 1 else vocab, tokens.data_ptr() if given else None, top, unit, lp.data_ptr() if given else None,
+                 H.data_ptr(), rank.data_ptr() if given else None, tt.data_ptr() if more else None, tl.data_ptr() if more else None)
+    ref, stream = C.byref(d), _stream_ptr()
+    need = _needs.get((rows, vocab, top))
+    if need is None:
+        n = C.c_uint64(0)
+        _check(lib().ead_logprobs_workspace(ref, C.byref(n)))
+        if len(_needs) >= 1024:
+            _needs.clear()
+        need = _needs[rows, vocab, top] = n.value
+    rc = lib().ead_logprobs(ref, _workspaces.get(need, device, stream) if need else None, need, stream)
+    if rc:
+        _check(rc)
     return LogProbs(H, lp, rank, tt, tl)
