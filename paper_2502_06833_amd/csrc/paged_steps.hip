@@ -195,9 +195,12 @@ ead_status ead_paged_weigh(const ead_paged_cache *cache, const ead_paged_batch *
     c.window = attn->window; c.sinks = attn->sinks;
     const int held = std::max(1, held_of(cache, batch));
     const hipStream_t st = (hipStream_t)hip_stream;
+    const long few_groups = (held + 128l * w.tiles - 1) / (128l * w.tiles) * cache->n_kv_heads, many_groups = (long)cache->n_kv_heads * w.m.splits * (w.m.part_keys / 256);
+    if ((w.few ? few_groups : many_groups) >= 1l << 24)
+        return refuse(EAD_ERR_SHAPE, "batch: max_kv of %d positions for each of %d KV heads needs 2^24 workgroups or more", batch->max_kv, cache->n_kv_heads);
     if (w.few) {
         c.tiles = w.tiles;
-        const dim3 grid((unsigned)((held + 128l * w.tiles - 1) / (128l * w.tiles) * cache->n_kv_heads), (unsigned)batch->batch);
+        const dim3 grid((unsigned)few_groups, (unsigned)batch->batch);
         with_cache(cache, [&](auto ct, auto hd) {
             using CT = decltype(ct);
             constexpr int HD = decltype(hd)::value;
@@ -208,7 +211,7 @@ ead_status ead_paged_weigh(const ead_paged_cache *cache, const ead_paged_batch *
     } else if (cache->dtype != EAD_F32 && c.q.vec) {
         c.splits = w.m.splits; c.part_keys = w.m.part_keys;
         c.part = (float *)workspace;
-        const dim3 grid((unsigned)((long)cache->n_kv_heads * w.m.splits * (w.m.part_keys / 256)), (unsigned)batch->batch);
+        const dim3 grid((unsigned)many_groups, (unsigned)batch->batch);
         with_cache(cache, [&](auto ct, auto hd) {
             using CT = decltype(ct);
             if constexpr (sizeof(CT) != 4) hipLaunchKernelGGL((k_weigh_many<CT, decltype(hd)::value>), grid, dim3(256), 0, st, c);
