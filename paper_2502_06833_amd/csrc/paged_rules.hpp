@@ -148,7 +148,7 @@ struct EvictPlan {
 inline EvictPlan evict_plan(int batch, int n_kv, int held, int keep, int recent, int vec_bytes, int cus) {
     EvictPlan p;
     const long units = (long)batch * n_kv, moves = std::max(0, std::min(held - keep, keep - recent));
-    p.threads = held > 4096 ? 1024 : 256;
+    p.threads = held > 4096 ? 1024 : held > 1024 ? 512 : 256;       // 64 sequences of 2176 positions: 19.5, 16.5 and 27 us with 256, 512 and 1024
     p.columns = 1;
     while (vec_bytes / p.columns > 64 && 2 * units * p.columns < 2l * cus) p.columns *= 2;
     p.shares = moves > 512 ? (int)std::max(1l, std::min(moves / 64, 8l * cus / (2 * units))) : 0;

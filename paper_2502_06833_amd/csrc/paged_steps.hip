@@ -54,7 +54,8 @@ ead_status check_weigh(const ead_paged_cache *cache, const ead_paged_batch *batc
     return EAD_OK;
 }
 
-int held_of(const ead_paged_cache *c, const ead_paged_batch *b) { return (int)std::min((long)b->max_kv, (long)b->table_width * c->page_size); }
+// positions of a sequence at most, as paged_seq cuts them
+int held_of(const ead_paged_cache *c, const ead_paged_batch *b) { return (int)std::min({(long)b->max_kv, (long)b->table_width * c->page_size, 0x7FFFFF00l}); }
 
 // LDS that k_evict_choose may use on the current device beside its own arrays
 int evict_room() {
