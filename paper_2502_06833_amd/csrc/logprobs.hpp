@@ -40,6 +40,10 @@ __device__ __forceinline__ float lp_bits(float l, float m) {
 }
 __device__ __forceinline__ float lp_rest(float m) { return lp_large(m) ? 0.f : __builtin_fmaf(m, kLpLog2e, -(m * kLpLog2e)); }
 
+__device__ __forceinline__ float lp_largest(const float (&f)[8]) {
+    return fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+}
+
 struct LpRun {
     float m, Z, S;
     int above;
@@ -204,12 +208,14 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
     run.init();
     int above = 0, of_group = 0, slot = 0;
     float best = -INFINITY;
-    auto take = [&](const Vec8<T> (&s)[kSetVecs]) {
+    float topA[kSetVecs], topB[kSetVecs];                      // the largest logits of the vectors in A and B
+    auto take = [&](const Vec8<T> (&s)[kSetVecs], float (&tops)[kSetVecs]) {
         float f[8], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kSetVecs; ++i) {
             s[i].unpack(f);
-            top = fmaxf(top, fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7]))));
+            tops[i] = lp_largest(f);
+            top = fmaxf(top, tops[i]);
         }
         const float m = fmaxf(run.m, top);
         run.move(m);
@@ -240,9 +246,9 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
         }
     };
     for (int set = begin; set < end; set += 8) {               // one in hand, the next on its way
-        take(A);
+        take(A, topA);
         if (set + 8 < end) row.load(A, set + 8, lane);
-        if (set + 4 < end) take(B);
+        if (set + 4 < end) take(B, topB);
         if (set + 12 < end) row.load(B, set + 12, lane);
     }
     if (TOP && of_group) s_best[wave][slot++][lane] = best;
@@ -261,29 +267,29 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
         s_lane[wave][lane] = lane_best;
         __syncthreads();
         const float bound = lp_kth<sizeof(T) == 2>(fmaxf(s_lane[0][lane], s_lane[1][lane]), fmaxf(s_lane[2][lane], s_lane[3][lane]), a.top);
+        const float least = fmaxf(bound, -3.402823466e38f);   // what is -inf is no candidate
         int found = 0;
-        auto collect = [&](const Vec8<T> (&s)[kSetVecs], int first_vec, bool in) {
+        auto collect = [&](const Vec8<T> (&s)[kSetVecs], const float (&tops)[kSetVecs], int first_vec) {
 #pragma unroll
             for (int i = 0; i < kSetVecs; ++i) {
+                if (!__any(tops[i] >= least)) continue;
                 float f[8];
                 s[i].unpack(f);
-                const float top = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
-                if (!__any(in && top >= bound)) continue;
                 const int first = (first_vec + i * 64) * 8 - row.shift;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) lp_collect(s_c[wave], found, f[e], first + e, in && f[e] >= bound && f[e] > -INFINITY, lane);
+                for (int e = 0; e < 8; ++e) lp_collect(s_c[wave], found, f[e], first + e, f[e] >= least, lane);
             }
         };
         // this wave's groups that reach the bound; two sets are still in registers
         int n = 0;
         if (sets <= 2) {
             slot = 0;
-            if (sets > 0) collect(A, begin * kSet + lane, true);
-            if (sets > 1) collect(B, (begin + 4) * kSet + lane, true);
+            if (sets > 0) collect(A, topA, begin * kSet + lane);
+            if (sets > 1) collect(B, topB, (begin + 4) * kSet + lane);
         }
         for (int i = 0; i < slot; ++i) {
             const float b = s_best[wave][i][lane];
-            const uint64_t hit = __ballot(b >= bound && b > -INFINITY);
+            const uint64_t hit = __ballot(b >= least);
             if (!hit) continue;
             const int at = n + __popcll(hit & ((1ull << lane) - 1));
             if ((hit >> lane & 1) && at < 64) s_group[wave][at] = i * 64 + lane;
@@ -294,13 +300,29 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
             const int id = lane < n ? s_group[wave][lane] : 0;
             for (int j = 0; j < each; ++j) {
                 const int at = (id >> 6) * each + j;           // the wave's set
+                const bool in = lane < n && at < sets;
                 Vec8<T> s[kSetVecs];
+                float tops[kSetVecs];
 #pragma unroll
                 for (int i = 0; i < kSetVecs; ++i) {
                     s[i].zero();
-                    if (lane < n && at < sets) row.load_one(s[i], (begin + 4 * at) * kSet + i * 64 + (id & 63));
+                    if (in) row.load_one(s[i], (begin + 4 * at) * kSet + i * 64 + (id & 63));
                 }
-                collect(s, (begin + 4 * at) * kSet + (id & 63), lane < n && at < sets);
+#pragma unroll
+                for (int i = 0; i < kSetVecs; ++i) {
+                    float f[8];
+                    s[i].unpack(f);
+                    tops[i] = in ? lp_largest(f) : -INFINITY;
+                }
+                if (least > 0.f || __all(in)) collect(s, tops, (begin + 4 * at) * kSet + (id & 63));
+                else                                           // (the zeros of lanes that have no group would count)
+#pragma unroll
+                    for (int i = 0; i < kSetVecs; ++i) {
+                        float f[8];
+                        s[i].unpack(f);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) lp_collect(s_c[wave], found, f[e], ((begin + 4 * at) * kSet + (id & 63) + i * 64) * 8 - row.shift + e, in && f[e] >= least, lane);
+                    }
             }
         }
         if (lane == 0) s_n[wave] = found;
@@ -313,7 +335,7 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
                 for (int i = 0; i < kSetVecs; ++i) {
                     float f[8];
                     A[i].unpack(f);
-                    const float top = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+                    const float top = lp_largest(f);
                     if (!__any(top > list.last(a.top) && top >= bound)) continue;
                     const int first = (at * kSet + i * 64 + lane) * 8 - row.shift;
 #pragma unroll 1
@@ -329,9 +351,11 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
         }
     }
     __syncthreads();
-    auto join_waves = [&] {                                    // by wave 0
+    auto join_sums = [&] {
         run.m = s_m[0]; run.Z = s_Z[0]; run.S = s_S[0]; run.above = s_above[0];
         for (int w = 1; w < 4; ++w) { LpRun o; o.m = s_m[w]; o.Z = s_Z[w]; o.S = s_S[w]; o.above = s_above[w]; run.add(o); }
+    };
+    auto join_lists = [&] {                                    // by wave 0
         if constexpr (TOP) {
             if (collected <= 64) {
                 int w = 0, at = lane;
@@ -351,19 +375,27 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
     };
     if (a.parts > 1) {
         const size_t at = (size_t)r * a.parts + part;
-        if (wave == 0) {
-            join_waves();
+        // wave 0 has the list, wave 1 the sums meanwhile (and without a list both)
+        if (wave == (TOP ? 1 : 0)) {
+            join_sums();
             if (lane == 0) {
                 LpPartial *p = a.stats + at;
                 st_coherent(&p->m, run.m); st_coherent(&p->Z, run.Z); st_coherent(&p->S, run.S); st_coherent(&p->above, run.above);
             }
-            if constexpr (TOP) {
+            wait_stores();
+        }
+        if constexpr (TOP) {
+            if (wave == 0) {
+                join_lists();
                 const int have = __popcll(__ballot(place < a.top));
                 const size_t to = (size_t)r * a.parts * a.top + part;
                 if (place < a.top) { st_coherent(a.list_value + to + place * a.parts, top_v); st_coherent(a.list_token + to + place * a.parts, top_t); }
                 if (lane >= have && lane < a.top) { st_coherent(a.list_value + to + lane * a.parts, -INFINITY); st_coherent(a.list_token + to + lane * a.parts, kNoIndex); }
+                wait_stores();
             }
-            wait_stores();
+            __syncthreads();
+        }
+        if (wave == 0) {
             if (lane == 0) {
                 int *ticket = a.tickets + (size_t)r * kLpTicketInts;
                 const bool last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.parts - 1;
@@ -430,7 +462,8 @@ __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
         for (int o = 32; o > 0; o >>= 1) run.above += __shfl_xor(run.above, o, kWave);
     } else {
         if (wave) return;
-        join_waves();
+        join_sums();
+        join_lists();
     }
     // nothing above -inf, or something that is no number: no distribution
     const bool some = run.Z > 0.f && run.Z < INFINITY;
