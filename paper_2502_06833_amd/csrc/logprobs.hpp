@@ -183,6 +183,12 @@ __device__ __forceinline__ int lp_place(float v, int t, int n, int lane) {
     return lane < n ? place : 64;
 }
 
+// One pass over a row: four waves take sets of 64 x 4 vectors in turn, one in hand and the next on its way; sums, the count of larger logits (scalar: a comparison
+// and a population count) and the largest are each lane's own until the end.  Rows that would leave compute units idle are cut into parts, and the last to arrive joins
+// them in their order (logprob_plan).  About 11 vector-issue slots a logit, exponential included: 2048 rows of 128256 bf16 logits 97 us (5.4 TB/s), 1023 of 50257 float32
+// 42.6 us (4.8 TB/s, every wave's start and end in it).  Small calls are latency: one row of 128256 with five alternatives 9.4 us, 64 rows of 151936 with twenty 16.2 us,
+// of which in the last workgroup 5 for the sums, 1.1 for the bound, 2 for the collection, 1.5 for the places, 1.1 for the ticket, 3.2 for the join; without alternatives 6.8
+// and 10.8.  (Lists that every wave kept sorted while it read took 10.9 and 43 us.)  All logits equal: 54 us for the 64 rows.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
     __shared__ float s_m[4], s_Z[4], s_S[4];

@@ -119,7 +119,9 @@ __device__ __forceinline__ void put16(void *pool, uint8_t *scales, size_t vec, i
 }
 
 // A group of HD / 16 lanes takes EACH heads of one kind (queries, keys, or values on their way to the pages) of a row, all of them requested before the first is worked
-// on; the row's sines and cosines are computed once for them, meanwhile.
+// on; the row's sines and cosines are computed once for them, meanwhile.  Bound by memory, with vector instructions (the sines above all) at two thirds of their rate
+// beside it: 16381 rows of 40 heads of 128 in bf16 73 us (4.6 TB/s; a large copy runs at 5.2), with values to bf16 pages, 28504 rows, 127 us (5.5 TB/s).  Four heads: eight took
+// 81 and 134 us (registers), one head in a loop 125 and 170.  STREAM: non-temporal accesses, for calls that move more than the second-level caches hold.
 struct RotateUnit {
     int kind, first, heads;              // 0: queries, 1: keys, 2: values; heads first .. first + heads - 1
 };
