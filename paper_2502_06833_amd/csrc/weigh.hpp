@@ -22,20 +22,21 @@ __device__ __forceinline__ bool weigh_sees(const PagedWeigh &c, int pos, int key
     return key <= pos && (!c.window || pos - key < c.window || key < c.sinks);
 }
 
-// A wave takes 16 keys against blocks of 16 rows (a row: a token and a head of the group): S = Q K^T with the rows as the M of the product and the keys as its N, so
-// that lane (n, g) = (lane & 15, lane >> 4) gets key n's scores of rows 4 g .. 4 g + 3 and adds their exponentials up by itself; the four g are added at the end.
+// A workgroup takes 16 keys, its waves every fourth block of 16 rows (a row: a token and a head of the group): S = Q K^T with the rows as the M of the product and the keys as its N, so
+// that lane (n, g) = (lane & 15, lane >> 4) gets key n's scores of rows 4 g .. 4 g + 3 and adds their exponentials up by itself; the four g, and then the waves in their order, are added at the end.
 // Every position has one owner: no atomics, and the sums' order is fixed.  Serves what the two kernels below do not: many rows of float32 models, and many whose queries do
-// not start on 16-byte boundaries (a piece of 2048 rows after 6145 positions, 32 heads: 1250 us here, 174 in k_weigh_many).
+// not start on 16-byte boundaries.  Latency: every block's queries are waited for (three float prompts of 500, 8 heads of 32: 18 us; 40 with a wave to 16 keys and all rows).
 template <typename CT, int HD>
 __global__ __launch_bounds__(256) void k_weigh(PagedWeigh c) {
     constexpr bool F32 = sizeof(CT) == 4;
     constexpr int KE = F32 ? 4 : 8, KL = HD / 4 / KE;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4, h = (int)blockIdx.y;
+    __shared__ float sums[4][16];
     const PagedSeq s = paged_seq(c.a, blockIdx.z);
     const int rows = s.n_rows * c.group;
     if (rows == 0) return;
-    for (int base = ((int)blockIdx.x * 4 + wave) * 16; base < s.kv; base += (int)gridDim.x * 64) {
+    for (int base = (int)blockIdx.x * 16; base < s.kv; base += (int)gridDim.x * 16) {
         const int page = __builtin_amdgcn_readfirstlane(paged_page(c.a, s, base));
         if (page < 0) continue;
         const int key = base + n;
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(256) void k_weigh(PagedWeigh c) {
             }
         }
         float sum = 0.f;
-        for (int r0 = 0; r0 < rows; r0 += 16) {
+        for (int r0 = wave * 16; r0 < rows; r0 += 64) {
             // rows before the first that reaches these keys see none of them, and with a window neither do those past its end
             const int p_hi = s.first + min(r0 + 15, rows - 1) / c.group, p_lo = s.first + r0 / c.group;
             if (p_hi < base || (c.window && p_lo - (base + 15) >= c.window && base >= c.sinks)) continue;
@@ -95,10 +96,13 @@ __global__ __launch_bounds__(256) void k_weigh(PagedWeigh c) {
         }
         sum += __shfl_xor(sum, 16, kWave);
         sum += __shfl_xor(sum, 32, kWave);
-        if (g == 0 && key < s.kv) {
+        if (g == 0) sums[wave][n] = sum;
+        __syncthreads();
+        if (wave == 0 && g == 0 && key < s.kv) {
             float *w = c.weights + vec;
-            *w = key < s.first ? *w + sum : sum;
+            *w = (key < s.first ? *w : 0.f) + (((sums[0][n] + sums[1][n]) + sums[2][n]) + sums[3][n]);
         }
+        __syncthreads();
     }
 }
 
@@ -297,8 +301,8 @@ __global__ __launch_bounds__(256, (WeighWave<CT, HD, NB>::kBlocks)) void k_weigh
 //   S = Q K^T with 32x32x16 products: lane (n, hh) = (lane & 31, lane >> 5) gets key n's scores of rows 8 i + 4 hh + 0..3 of a tile, i = 0..3, and adds their
 //   exponentials up; the halves of the wave are added at the end.
 // The rows that see a tile of keys are cut into c.splits ranges; with more than one each leaves its sums for k_weigh_join.
-// A score takes an fma, an exponential (a quarter-rate instruction) and an addition, 24 cycles a wave beside 16 of products: 2048 rows after 6145 positions, 32 heads of 128, 182 us with the
-// join's 5 (690 Tflop/s), matrix cores 37 % busy, vector issue 62 % and the exponentials' further cycles on top.  The next tile's products between this one's exponentials
+// A score takes an fma, an exponential (a quarter-rate instruction) and an addition, 24 cycles a wave beside 16 of products: 2048 rows after 6145 positions, 32 heads of 128, 170 us with the
+// join's 5 (716 Tflop/s), matrix cores 37 % busy, vector issue 62 % and the exponentials' further cycles on top.  The next tile's products between this one's exponentials
 // (registers for two waves to a SIMD instead of three) took 213 us, all of a tile's queries read before its products as long as this.
 template <typename CT, int HD>
 __global__ __launch_bounds__(256, 2) void k_weigh_many(PagedWeigh c) {
@@ -342,18 +346,18 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(PagedWeigh c) {
     const uint32_t base = lds_address(lds);
     constexpr int kPieces = kReq > 0 ? kReq : 1;
     const bool asks = kReq > 0 || wave < 2;
-    int rem[kPieces], row_at[kPieces];
+    int rem[kPieces], row_of[kPieces];
     const bf16_t *from[kPieces];
     const int step_tok = 32 / c.group, step_rem = 32 % c.group;
     const long step = step_tok * c.q.row_stride + step_rem * c.q.head_stride, wrap = c.q.row_stride - c.group * c.q.head_stride;
     const bf16_t *first_row = (const bf16_t *)c.q.p + (size_t)s.row0 * c.q.row_stride + (size_t)(h * c.group) * c.q.head_stride;
 #pragma unroll
     for (int e = 0; e < kPieces; ++e) {
-        const int at = (kReq > 0 ? wave * kReq + e : wave & 1) * 1024 + lane * 16, r = at / kRowBytes;
-        row_at[e] = t0 * 32 + r;
-        const int tok = row_at[e] / c.group;
-        rem[e] = row_at[e] % c.group;
-        from[e] = first_row + tok * c.q.row_stride + rem[e] * c.q.head_stride + ((at % kRowBytes >> 4) ^ lds_swizzle<kRowBytes>(r)) * 8;
+        const int at = (kReq > 0 ? wave * kReq + e : wave & 1) * 1024 + lane * 16;
+        row_of[e] = at / kRowBytes;
+        const int r = t0 * 32 + row_of[e], tok = r / c.group;
+        rem[e] = r % c.group;
+        from[e] = first_row + tok * c.q.row_stride + rem[e] * c.q.head_stride + ((at % kRowBytes >> 4) ^ lds_swizzle<kRowBytes>(row_of[e])) * 8;
     }
     int z_row = t0 * 32 + lane, z_tok = z_row / c.group, z_rem = z_row % c.group;          // wave 0, lanes 0 .. 31: the tile's lse
     auto request = [&](int t) {
@@ -361,16 +365,20 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(PagedWeigh c) {
         if (!asks) return;
 #pragma unroll
         for (int e = 0; e < kPieces; ++e) {
-            request_pieces(row_at[e] < rows ? from[e] : first_row, to + e * 1024);         // past the last row: a row whose scores are left out
-            row_at[e] += 32;
-            rem[e] += step_rem;
-            from[e] += step + (rem[e] >= c.group ? wrap : 0);
-            rem[e] -= rem[e] >= c.group ? c.group : 0;
+            if (t * 32 + 32 <= rows) request_pieces(from[e], to + e * 1024);
+            else request_pieces(t * 32 + row_of[e] < rows ? from[e] : first_row, to + e * 1024);       // past the last row: a row whose scores are left out
+            from[e] += step;
+            if (step_rem) {
+                rem[e] += step_rem;
+                from[e] += rem[e] >= c.group ? wrap : 0;
+                rem[e] -= rem[e] >= c.group ? c.group : 0;
+            }
         }
     };
     auto next_lse = [&] {
         float z = -INFINITY;
-        if (wave == 0 && lane < 32 && z_row < rows) z = c.lse[(size_t)(s.row0 + z_tok) * c.n_heads + h * c.group + z_rem];
+        if (wave) return z;
+        if (lane < 32 && z_row < rows) z = c.lse[(size_t)(s.row0 + z_tok) * c.n_heads + h * c.group + z_rem];
         z_row += 32;
         z_tok += step_tok;
         z_rem += step_rem;
