@@ -36,7 +36,8 @@ __global__ __launch_bounds__(256) void k_weigh(PagedWeigh c) {
     const PagedSeq s = paged_seq(c.a, blockIdx.z);
     const int rows = s.n_rows * c.group;
     if (rows == 0) return;
-    for (int base = (int)blockIdx.x * 16; base < s.kv; base += (int)gridDim.x * 16) {
+    const int step = (int)gridDim.x * 16;
+    for (int base = (int)blockIdx.x * 16; base < s.kv; base = s.kv - base > step ? base + step : s.kv) {       // (a sum past 2^31 would start over)
         const int page = __builtin_amdgcn_readfirstlane(paged_page(c.a, s, base));
         if (page < 0) continue;
         const int key = base + n;
