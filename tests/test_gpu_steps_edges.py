@@ -162,3 +162,35 @@ def test_rotation_of_a_row_back_and_forth():
         size = (x[..., :64].abs() + x[..., 64:].abs()).repeat(1, 1, 2)
         assert bool(((x - y).abs() <= 4 * 20 * 2.0 ** -24 * size).all())
     check_rotated(rot(q, k, p)[0], q, None, p, rot.inv_freq)
+
+
+@pytest.mark.parametrize("n,keep,sinks,recent,ties", [(1 << 20, 600001, 5, 77, False), (1 << 20, 300000, 0, 250000, True), (200001, 100000, 16, 33, False), (70000, 35000, 1, 0, True),
+                                                      (1 << 20, (1 << 20) - 3, 0, 1, True)])
+def test_evict_the_longest_sequences(n, keep, sinks, recent, ties):
+    """Sequences whose scores, and whose lists of moves, do not fit a workgroup's local memory."""
+    page, per = 256, -(-n // 256)
+    g = torch.Generator(device=DEV); g.manual_seed(n + keep)
+    cache = ead.PagedCache.empty(per, page, 1, 32, F8)
+    cache.k_pages.view(torch.uint8).random_(0, 256, generator=g), cache.v_pages.view(torch.uint8).random_(0, 256, generator=g)
+    cache.k_scales.random_(1, 255, generator=g), cache.v_scales.random_(1, 255, generator=g)
+    table = torch.randperm(per, generator=g, device=DEV).to(torch.int32)[None]
+    batch = ead.PagedBatch.of(table, [0], [n])
+    scores = torch.randn(per, 1, page, generator=g, device=DEV).exp()
+    if ties:
+        scores = (scores * 2).round()
+    at = torch.arange(n, device=DEV)
+    place = lambda p: (table[0].long()[p // page], 0, p % page)  # noqa: E731
+    old = [t.view(torch.uint8)[place(at)].clone() for t in (cache.k_pages, cache.v_pages)] + [t[place(at)].clone() for t in (cache.k_scales, cache.v_scales, scores)]
+    stay, cut = keep - sinks - recent, keep - recent
+    chosen = torch.zeros(n, dtype=torch.bool, device=DEV)
+    chosen[torch.sort(old[4][sinks:n - recent], descending=True, stable=True).indices[:stay] + sinks] = True
+    want = at[:keep].clone()
+    want[cut:] = at[n - recent:]
+    free = (~chosen[:cut] & (at[:cut] >= sinks)).nonzero()[:, 0]
+    late = chosen[cut:].nonzero()[:, 0] + cut
+    assert free.numel() == late.numel() and (free.numel() > 40000 or keep > 10 ** 6 or n < 10 ** 6)
+    want[free] = late
+    kept = cache.evict(batch, scores, keep, sinks=sinks, recent=recent)
+    assert torch.equal(kept[0, 0].long(), want)
+    now = [t.view(torch.uint8)[place(at[:keep])] for t in (cache.k_pages, cache.v_pages)] + [t[place(at[:keep])] for t in (cache.k_scales, cache.v_scales, scores)]
+    assert all(torch.equal(a, b[want]) for a, b in zip(now, old))
