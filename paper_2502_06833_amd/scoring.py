@@ -25,7 +25,8 @@ class LogProbs(NamedTuple):
 
 class _Workspaces:
     """One for each stream, cleared when it is made; calls leave it ready for the next.  A capture's calls have one for each of its streams, in the graph's memory and
-    cleared by a node of the graph."""
+    cleared by a node of the graph.  Threads share them: a call holds the tensor that it got until its kernel is launched, since another thread's call on the same
+    stream may meanwhile put a larger one in its place (after that the stream's order keeps them apart)."""
 
     def __init__(self):
         self._eager, self._captured = {}, (None, {})
@@ -42,7 +43,7 @@ class _Workspaces:
         if ws is None or ws.numel() * 4 < need:
             import torch
             ws = of[key] = torch.zeros((need + 3) // 4, dtype=torch.int32, device=torch.device("cuda", device))
-        return ws.data_ptr()
+        return ws
 
 
 _workspaces = _Workspaces()
@@ -87,7 +88,8 @@ def logprobs(logits, tokens=None, top=0, unit=NATS):
         if len(_needs) >= 1024:
             _needs.clear()
         need = _needs[rows, vocab, top] = n.value
-    rc = lib().ead_logprobs(ref, _workspaces.get(need, device, stream) if need else None, need, stream)
+    ws = _workspaces.get(need, device, stream) if need else None
+    rc = lib().ead_logprobs(ref, ws.data_ptr() if need else None, need, stream)
     if rc:
         _check(rc)
     return LogProbs(H, lp, rank, tt, tl)
