@@ -36,9 +36,10 @@ class _Workspaces:
         if paged._capturing():
             n = C.c_uint64(0)
             _check(lib().ead_stream_capture(C.c_void_p(stream), C.byref(n)))
-            if self._captured[0] != (device, n.value):
-                self._captured = ((device, n.value), {})
-            of = self._captured[1]
+            captured = self._captured                          # (read once: another thread's capture may replace it)
+            if captured[0] != (device, n.value):
+                captured = self._captured = ((device, n.value), {})
+            of = captured[1]
         ws = of.get(key)
         if ws is None or ws.numel() * 4 < need:
             import torch

@@ -82,3 +82,26 @@ def test_a_workspace_lives_until_its_launch(made, monkeypatch, capturing, first,
     assert sorted(rows for rows, _, _ in L.seen) == sorted((first, second))
     for rows, at, size in L.seen:                             # every launch got as much as it asked for
         assert size == 4096 * rows and any(at == a and n >= size for a, n, _ in made)
+
+
+def test_captures_of_two_threads_do_not_mix(made, monkeypatch):
+    """A second capture that begins between a call's look at the captures and its workspace's place among them: none gets the other's memory."""
+    w = scoring._workspaces
+    monkeypatch.setattr(paged, "_capturing", lambda: True)
+    L = Library(None)
+    monkeypatch.setattr(scoring, "lib", lambda: L)
+
+    class Slot(tuple):
+        """A capture's workspaces whose first look lets another thread's capture in."""
+
+        def __getitem__(self, i):
+            if Slot.meanwhile:
+                run, Slot.meanwhile = Slot.meanwhile, None
+                run()
+            return tuple.__getitem__(self, i)
+
+    w.get(64, 0, 1)
+    w._captured = Slot(w._captured)
+    Slot.meanwhile = lambda: w.get(64, 0, 2)
+    w.get(64, 0, 1)
+    assert w._captured[0] == (0, 2) and set(w._captured[1]) == {(0, 2)}
