@@ -117,6 +117,9 @@ inline bool rotate_streams(long rows, long heads, int head_dim, int bytes) { ret
 // Sequences of up to this many rows per KV head (new tokens times query heads per KV head) keep their queries in registers while keys stream past (k_weigh_few); with more
 // the keys stay and the rows stream (k_weigh_many).  Float queries take twice the registers.
 constexpr int weigh_few_rows(bool f32, int head_dim) { return f32 && head_dim == 128 ? 32 : 64; }
+// Workgroups of k_weigh for a KV head of a sequence: 16 keys each, and past 2^24 positions again 2^24 further on (a launch counts its threads in 32 bits: from 2^28 positions on
+// one workgroup to every 16 keys would not fit)
+inline unsigned weigh_simple_groups(int held) { return (unsigned)std::min((held + 15l) / 16, 1l << 20); }
 // Tiles of 32 keys to a wave of k_weigh_few: eight at most, since sequences are of different lengths (64 sequences: 114 us with 8, 120 with 16)
 inline int weigh_tiles(long units, int held, int cus) {
     const long groups = units * std::max(1, (held + 127) / 128);

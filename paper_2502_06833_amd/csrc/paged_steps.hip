@@ -220,7 +220,7 @@ ead_status ead_paged_weigh(const ead_paged_cache *cache, const ead_paged_batch *
         if (w.m.splits > 1)
             hipLaunchKernelGGL(k_weigh_join, dim3((unsigned)(w.m.part_keys / 256), (unsigned)cache->n_kv_heads, (unsigned)batch->batch), dim3(256), 0, st, c);
     } else {
-        const dim3 grid((unsigned)((held + 15l) / 16), (unsigned)cache->n_kv_heads, (unsigned)batch->batch);
+        const dim3 grid(weigh_simple_groups(held), (unsigned)cache->n_kv_heads, (unsigned)batch->batch);
         with_cache(cache, [&](auto ct, auto hd) { hipLaunchKernelGGL((k_weigh<decltype(ct), decltype(hd)::value>), grid, dim3(256), 0, st, c); });
     }
     return launched("ead_paged_weigh");
