@@ -384,7 +384,9 @@ ead_status ead_paged_append(const ead_paged_cache *cache, const ead_paged_batch 
  * with the arguments and the lse of ead_paged_attention for the same rows (lse [rows][n_heads]; a row whose lse is -infinity pays
  * nothing).  New positions start from nothing, so pages need no clearing where every step's rows are weighed.  Sums are
  * float32, in an order that the call's sizes fix (no atomics).  A page belongs to one sequence of the batch: what two sequences
- * of a call pay to a page they share is not added up right.  attn->one_term is not looked at.  Positions past max_kv may get
+ * of a call pay to a page they share is not added up right.  Weights of positions that no row sees (a window has passed them) are
+ * not written, so a table may go on naming pages that a window has left behind and that have gone to other sequences.  A window
+ * does not shorten the call: all keys of a sequence are read.  attn->one_term is not looked at.  Positions past max_kv may get
  * nothing, and rows beyond max_q may pay nothing.  Workspaces as those of ead_paged_attention, but nothing has to clear them. */
 ead_status ead_paged_weigh_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_attn *attn,
                                      uint64_t *bytes);

@@ -22,6 +22,11 @@ __device__ __forceinline__ bool weigh_sees(const PagedWeigh &c, int pos, int key
     return key <= pos && (!c.window || pos - key < c.window || key < c.sinks);
 }
 
+// Whether any row sees a key.  What a window has passed is not written at all: its weight stays as it is, and its page may be another sequence's by now, with an owner of its own
+__device__ __forceinline__ bool weigh_seen(const PagedWeigh &c, const PagedSeq &s, int key) {
+    return !c.window || key < c.sinks || max(s.first, 0) - key < c.window;
+}
+
 // A workgroup takes 16 keys, its waves every fourth block of 16 rows (a row: a token and a head of the group): S = Q K^T with the rows as the M of the product and the keys as its N, so
 // that lane (n, g) = (lane & 15, lane >> 4) gets key n's scores of rows 4 g .. 4 g + 3 and adds their exponentials up by itself; the four g, and then the waves in their order, are added at the end.
 // Every position has one owner: no atomics, and the sums' order is fixed.  Serves what the two kernels below do not: many rows of float32 models, and many whose queries do
@@ -99,7 +104,7 @@ __global__ __launch_bounds__(256) void k_weigh(PagedWeigh c) {
         sum += __shfl_xor(sum, 32, kWave);
         if (g == 0) sums[wave][n] = sum;
         __syncthreads();
-        if (wave == 0 && g == 0 && key < s.kv) {
+        if (wave == 0 && g == 0 && key < s.kv && weigh_seen(c, s, key)) {
             float *w = c.weights + vec;
             *w = (key < s.first ? *w : 0.f) + (((sums[0][n] + sums[1][n]) + sums[2][n]) + sums[3][n]);
         }
@@ -281,7 +286,7 @@ __global__ __launch_bounds__(256, (WeighWave<CT, HD, NB>::kBlocks)) void k_weigh
         const int key = base + 16 * (lane >> 5) + n, page = __builtin_amdgcn_readlane(pages, 2 * i), page_too = __builtin_amdgcn_readlane(pages, 2 * i + 1);
         const int mine = lane & 32 ? page_too : page;
         const float old = lds_read<float>(at + W::kKeys + 64 * (lane >> 5) + 4 * n);
-        if (!(lane & 16) && mine >= 0 && key < s.kv) c.weights[paged_vec(c.a, mine, h, key & page_mask)] = (key < s.first ? old : 0.f) + paid;
+        if (!(lane & 16) && mine >= 0 && key < s.kv && (!EDGE || weigh_seen(c, s, key))) c.weights[paged_vec(c.a, mine, h, key & page_mask)] = (key < s.first ? old : 0.f) + paid;
     };
 #pragma unroll
     for (int i = 0; i < W::kRing - 1; ++i)
@@ -459,7 +464,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(PagedWeigh c) {
         const int key = my0 + 32 * b + n;
         if (hh == 0 && live[b]) {
             if (c.splits > 1) c.part[(((size_t)split * gridDim.y + blockIdx.y) * c.a.n_kv + h) * c.part_keys + key] = sum[b];
-            else c.weights[vec[b]] = (key < s.first ? c.weights[vec[b]] : 0.f) + sum[b];
+            else if (weigh_seen(c, s, key)) c.weights[vec[b]] = (key < s.first ? c.weights[vec[b]] : 0.f) + sum[b];
         }
     }
 }
@@ -470,7 +475,7 @@ __global__ __launch_bounds__(256) void k_weigh_join(PagedWeigh c) {
     const PagedSeq s = paged_seq(c.a, blockIdx.z);
     if (s.n_rows == 0 || key >= min(s.kv, c.part_keys)) return;
     const int page = paged_page(c.a, s, key);
-    if (page < 0) return;
+    if (page < 0 || !weigh_seen(c, s, key)) return;
     float *w = c.weights + paged_vec(c.a, page, h, key & ((1 << c.a.page_shift) - 1));
     float sum = key < s.first ? *w : 0.f;
     const size_t apart = (size_t)gridDim.z * c.a.n_kv * c.part_keys;

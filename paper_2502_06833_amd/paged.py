@@ -366,7 +366,8 @@ class PagedCache:
     def weigh(self, q, lse, batch, weights, window=0, sinks=0, scale=None):
         """Adds to `weights` (float32 [n_pages, n_kv_heads, page_size], see new_weights) what the rows' attention pays to every position
         they see, exp(scale q k - lse) over the rows and the query heads of a group; the rows' own positions start from nothing.  q, window, sinks and
-        scale as for `attention` of the same rows, lse as it returned it.  A page belongs to one sequence of the batch."""
+        scale as for `attention` of the same rows, lse as it returned it.  A page belongs to one sequence of the batch; weights of positions
+        that a window has passed are left alone (their pages may be others' by now), though their keys are still read."""
         if q.dim() != 3:
             raise ValueError(f"q: expected [rows, n_heads, {self.head_dim}], got {list(q.shape)}")
         if _code(q) != (F32 if self._code == F32 else BF16):
