@@ -236,7 +236,7 @@ ead_status ead_paged_evict_workspace(const ead_paged_cache *cache, const ead_pag
         return refuse(EAD_ERR_INVALID_ARG, "eviction: need keep >= 1, sinks >= 0, recent >= 0 and sinks + recent <= keep");
     if (held_of(cache, batch) > kEvictMost) return refuse(EAD_ERR_SHAPE, "batch: sequences of up to 2^20 positions can be cut, max_kv is %d", batch->max_kv);
     const uint64_t units = (uint64_t)batch->batch * cache->n_kv_heads;
-    *bytes = evict_moves_at(units) + units * (uint64_t)(ev->keep - ev->sinks - ev->recent) * 8;
+    *bytes = evict_moves_at(units) + (held_of(cache, batch) > ev->keep ? units * (uint64_t)(ev->keep - ev->sinks - ev->recent) * 8 : 0);      // (moves: only where something is cut)
     return EAD_OK;
 }
 
