@@ -215,7 +215,7 @@ __device__ __forceinline__ void evict_choose(const PagedEvict &c, const PagedSeq
 }
 
 __global__ __launch_bounds__(kEvictThreads) void k_evict_choose(PagedEvict c) {
-    extern __shared__ uint32_t lds[];                     // ranks of the first c.cached positions, then a bit for every position
+    extern __shared__ __align__(16) uint32_t lds[];       // ranks of the first c.cached positions (written four at a time), then a bit for every position, 64 to a word
     __shared__ int bins[kEvictBins];
     __shared__ int part[17], found[3];
     const int h = (int)blockIdx.x, b = (int)blockIdx.y;
