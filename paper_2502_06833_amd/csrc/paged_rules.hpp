@@ -106,12 +106,11 @@ inline PagedPlan paged_many(int batch, int n_kv, int group, long rows, int max_k
 }
 
 // ---- rotation ----
-// Heads of a row that a group of lanes takes: one while that does not fill the device, then four, which share sines and cosines and are requested together
+// Heads of a row that a group of lanes takes: one while that does not fill the device, then four, which share sines and cosines and are requested together.  Calls that are
+// wide move 67 MB and more, so that none of it stays in the second-level caches (32 MB): their accesses are non-temporal.
 constexpr int kRotateEach = 4;
 inline bool rotate_wide(long rows, long heads, int head_dim) { return rows * heads * (head_dim / 16) > 4l * 256 * 1024; }
 inline long rotate_units(long q, long k, long v, int each) { return (q + each - 1) / each + (k + each - 1) / each + (v + each - 1) / each; }
-// Whether a call moves more than stays in the second-level caches
-inline bool rotate_streams(long rows, long heads, int head_dim, int bytes) { return 2.0 * rows * heads * head_dim * bytes > 64e6; }
 
 // ---- weighing ----
 // Sequences of up to this many rows per KV head (new tokens times query heads per KV head) keep their queries in registers while keys stream past (k_weigh_few); with more
