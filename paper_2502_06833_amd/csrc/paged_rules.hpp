@@ -106,10 +106,14 @@ inline PagedPlan paged_many(int batch, int n_kv, int group, long rows, int max_k
 }
 
 // ---- rotation ----
-// Heads of a row that a group of lanes takes: one while that does not fill the device, then four, which share sines and cosines and are requested together.  Calls that are
-// wide move 67 MB and more, so that none of it stays in the second-level caches (32 MB): their accesses are non-temporal.
+// Heads of a row that a group of lanes takes: one, or of many bf16 rows four, which share sines and cosines and are requested together.  Such calls move 67 MB and more, none of
+// which stays in the second-level caches (32 MB), so their accesses are non-temporal.  Inputs from memory, 32 and 8 heads, four against one: heads of 128, 816 rows 8.7 and 9.3 us, 3272
+// rows (the bound) 18.5 and 26.9, 26208 rows 114 and 173; of 64, 6552 rows (the bound) 21.8 and 27.2.  Where a call just before left its inputs in the last-level cache the two cross
+// about the bound (heads of 64, 6552 rows: 22.7 and 21.2; of 128, 2048: 10.8 and 14.6).  One is the faster where vectors are short or wide: heads of 32, 32768 rows of 16, 35 and 27 us; float32,
+// 8 requests of 32 bytes to a lane: heads of 128, 6552 rows 62.5 and 60.0, prompts to 8 bits 115 and 101; heads of 32 49 and 35.
 constexpr int kRotateEach = 4;
-inline bool rotate_wide(long rows, long heads, int head_dim) { return rows * heads * (head_dim / 16) > 4l * 256 * 1024; }
+constexpr bool rotate_shares(int bytes, int head_dim) { return bytes == 2 && head_dim >= 64; }
+inline bool rotate_wide(long rows, long heads, int head_dim, int bytes) { return rotate_shares(bytes, head_dim) && rows * heads * (head_dim / 16) > 4l * 256 * 1024; }
 inline long rotate_units(long q, long k, long v, int each) { return (q + each - 1) / each + (k + each - 1) / each + (v + each - 1) / each; }
 
 // ---- weighing ----

@@ -116,7 +116,7 @@ ead_status ead_rotate(const ead_rotary *rotary, int32_t dtype, int32_t rows, int
     c.positions = positions;
     c.n_heads = n_heads; c.n_kv = n_kv_heads;
     const long total = (long)n_heads + n_kv_heads, per_group = 256 / (rotary->head_dim / 16);
-    const bool wide = rotate_wide(rows, total, rotary->head_dim);
+    const bool wide = rotate_wide(rows, total, rotary->head_dim, element_bytes(dtype));
     c.groups = (int)rotate_units(n_heads, n_kv_heads, 0, wide ? kRotateEach : 1);
     const dim3 grid((unsigned)std::clamp(((long)rows * c.groups + per_group - 1) / per_group, 1l, 1l << 20));       // the kernel goes on past its grid
     with_head_dim(rotary->head_dim, [&](auto hd) {
@@ -124,7 +124,7 @@ ead_status ead_rotate(const ead_rotary *rotary, int32_t dtype, int32_t rows, int
         auto go = [&](auto rt) {
             using RT = decltype(rt);
             if (!wide) hipLaunchKernelGGL((k_rotate<RT, HD, 1, false>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
-            else hipLaunchKernelGGL((k_rotate<RT, HD, kRotateEach, true>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
+            else if constexpr (rotate_shares(sizeof(RT), HD)) hipLaunchKernelGGL((k_rotate<RT, HD, kRotateEach, true>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
         };
         if (dtype == EAD_F32) go(0.f);
         else go(bf16_t{});
@@ -149,7 +149,7 @@ ead_status ead_paged_append(const ead_paged_cache *cache, const ead_paged_batch 
     c.a = args_of(cache, batch);
     c.positions = positions;
     c.n_heads = n_heads; c.n_kv = cache->n_kv_heads;
-    const bool wide = rotate_wide(batch->rows, total, cache->head_dim);
+    const bool wide = rotate_wide(batch->rows, total, cache->head_dim, element_bytes(dtype));
     c.groups = (int)rotate_units(n_heads, cache->n_kv_heads, cache->n_kv_heads, wide ? kRotateEach : 1);
     const long per_group = 256 / (cache->head_dim / 16);
     const dim3 grid((unsigned)std::clamp(((long)batch->max_q * c.groups + per_group - 1) / per_group, 1l, 1l << 20), (unsigned)batch->batch);
@@ -159,7 +159,7 @@ ead_status ead_paged_append(const ead_paged_cache *cache, const ead_paged_batch 
         auto go = [&](auto rt) {
             using RT = decltype(rt);
             if (!wide) hipLaunchKernelGGL((k_append<CT, RT, HD, 1, false>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
-            else hipLaunchKernelGGL((k_append<CT, RT, HD, kRotateEach, true>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
+            else if constexpr (rotate_shares(sizeof(RT), HD)) hipLaunchKernelGGL((k_append<CT, RT, HD, kRotateEach, true>), grid, dim3(256), 0, (hipStream_t)hip_stream, c);
         };
         if (dtype == EAD_F32) go(0.f);
         else go(bf16_t{});
