@@ -186,9 +186,10 @@ class PagedBatch:
         """The plans of the capture under way: they go with the next one, and their memory is the graph's until then and after."""
         n = C.c_uint64(0)
         _check(lib().ead_stream_capture(C.c_void_p(stream), C.byref(n)))
-        if self._of_capture[0] != n.value:
-            self._of_capture = (n.value, {})
-        return self._of_capture[1]
+        of = self._of_capture                                 # (read once: another thread's capture of the batch may replace it)
+        if of[0] != n.value:
+            of = self._of_capture = (n.value, {})
+        return of[1]
 
     def _plan(self, cache, n_heads, window, sinks, scale, one_term, stream):
         """The attention arguments, and the workspace of this stream: cleared once, then every call leaves it ready for the next."""
