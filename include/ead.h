@@ -387,7 +387,8 @@ ead_status ead_paged_append(const ead_paged_cache *cache, const ead_paged_batch 
  * of a call pay to a page they share is not added up right.  Weights of positions that no row sees (a window has passed them) are
  * not written, so a table may go on naming pages that a window has left behind and that have gone to other sequences.  A window
  * does not shorten the call: all keys of a sequence are read.  attn->one_term is not looked at.  Positions past max_kv may get
- * nothing, and rows beyond max_q may pay nothing.  Workspaces as those of ead_paged_attention, but nothing has to clear them. */
+ * nothing, and rows beyond max_q may pay nothing.  n_kv_heads * max_kv of 2^32 and more may be refused (EAD_ERR_SHAPE).  Workspaces
+ * as those of ead_paged_attention, but nothing has to clear them. */
 ead_status ead_paged_weigh_workspace(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_attn *attn,
                                      uint64_t *bytes);
 ead_status ead_paged_weigh(const ead_paged_cache *cache, const ead_paged_batch *batch, const ead_paged_attn *attn,

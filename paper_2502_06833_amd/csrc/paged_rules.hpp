@@ -118,17 +118,21 @@ inline long rotate_units(long q, long k, long v, int each) { return (q + each - 
 
 // ---- weighing ----
 // Sequences of up to this many rows per KV head (new tokens times query heads per KV head) keep their queries in registers while keys stream past (k_weigh_few); with more
-// the keys stay and the rows stream (k_weigh_many).  Float queries take twice the registers.
+// the keys stay and the rows stream (k_weigh_many).  Float queries take twice the registers.  Few against many, 8 KV heads: heads of 128, one sequence of 8192 bf16 keys, 16 rows 5.3 and
+// 7.6 us, 32 6.6 and 7.5, 64 10.2 and 10.0; sixteen of 4096 26 and 32, 29.5 and 28.9, 41 and 34; of 8-bit ones 16 and 30, 20 and 28, 37 and 33; heads of 64, bf16, 14 and 20, 16 and 19, 28
+// and 24.  So 64 rows are past the crossing where there are many keys, and on it for one sequence.
 constexpr int weigh_few_rows(bool f32, int head_dim) { return f32 && head_dim == 128 ? 32 : 64; }
 // Workgroups of k_weigh for a KV head of a sequence: 16 keys each, and past 2^24 positions again 2^24 further on (a launch counts its threads in 32 bits: from 2^28 positions on
 // one workgroup to every 16 keys would not fit)
 inline unsigned weigh_simple_groups(int held) { return (unsigned)std::min((held + 15l) / 16, 1l << 20); }
-// Tiles of 32 keys to a wave of k_weigh_few: eight at most, since sequences are of different lengths (64 sequences: 114 us with 8, 120 with 16)
+// Tiles of 32 keys to a wave of k_weigh_few: eight at most, since sequences are of different lengths (64 of 1024 to 16384 8-bit keys: 102, 74, 68, 70, 80 and 98 us with at most 1, 2, 4, 8,
+// 16 and 32; 64 of 4096: 73, 52, 48, 49, 49 and 49; 16 of 8192 bf16 keys: 62, 47, and 42 from 4 on)
 inline int weigh_tiles(long units, int held, int cus) {
     const long groups = units * std::max(1, (held + 127) / 128);
     return (int)std::max(1l, std::min(8l, (groups + 8l * cus - 1) / (8l * cus)));
 }
-// Ranges of rows of k_weigh_many, and the keys that a range's sums are kept for (a piece of 2048 rows: 224, 204 and 194 us with 3, 6 and 12 workgroups for every compute unit)
+// Ranges of rows of k_weigh_many, and the keys that a range's sums are kept for.  With 1, 3, 6, 12 and 24 workgroups for every compute unit (bf16, 32 and 8 heads): 2048 rows of 8193 keys 304,
+// 194, 181, 168 and 156 us; 512 rows of 8193 118, 80, 64, 61 and 61; 2048 of 2048 118, 70, 47, 50 and 50; four times 1024 of 4096 272, 285, 243, 221 and 211.  (24 would hold twice the sums.)
 struct WeighPlan { int splits, part_keys; };
 inline WeighPlan weigh_many(int batch, int n_kv, long rows, int held, int cus) {
     WeighPlan p;
@@ -154,7 +158,10 @@ struct EvictPlan {
 inline EvictPlan evict_plan(int batch, int n_kv, int held, int keep, int recent, int vec_bytes, int cus) {
     EvictPlan p;
     const long units = (long)batch * n_kv, moves = std::max(0, std::min(held - keep, keep - recent));
-    p.threads = held > 4096 ? 1024 : held > 1024 ? 512 : 256;       // 64 sequences of 2176 positions: 19.5, 16.5 and 27 us with 256, 512 and 1024
+    // Whole evictions with 256, 512 and 1024 threads, 8 heads: 64 sequences of 700 positions 38.7, 37.3 and 45.9 us, of 2176 48, 46 and 54, of 4000 54, 50 and 59, of 8000 67, 58 and 66;
+    // three of 2176 17.8, 15.3 and 16.1, of 8000 30, 22 and 21, of 16000 69, 51 and 46, of 28000 111, 79 and 69.  1024 are the faster ones where few sequences are long; `held` is the
+    // caller's bound, so one that is far above the lengths takes them too (64 of 700 under a bound of 16384: 45.3, with 512 37.4).
+    p.threads = held > 4096 ? 1024 : held > 1024 ? 512 : 256;
     p.columns = 1;
     while (vec_bytes / p.columns > 64 && 2 * units * p.columns < 2l * cus) p.columns *= 2;
     p.shares = moves > 512 ? (int)std::max(1l, std::min(moves / 64, 8l * cus / (2 * units))) : 0;
@@ -165,7 +172,9 @@ inline EvictPlan evict_plan(int batch, int n_kv, int held, int keep, int recent,
 // ---- log probabilities ----
 // Workgroups of four waves that a row of logits goes to, and sets of `set` vectors to each (a row that does not start on a 16-byte boundary has up to one vector more)
 struct LogprobPlan { int parts, part_sets; };
-constexpr long kLogprobTarget = 4;         // workgroups for every compute unit (64 rows of 151936: 22.2, 20.9, 21.3 and 27.5 us with 1, 2, 4 and 8)
+// Workgroups for every compute unit.  1, 2, 4 and 8: 64 rows of 151936 with twenty alternatives 18.3, 17.0, 16.4 and 20.4 us, without 12.6, 11.6, 11.3 and 12.8; 512 of 128256 without 32.7, 31.4,
+// 30.3 and 32.7; 300 of 50257 with five 20.4, 20.3, 22.5 and 23.1; fewer or shorter rows are cut into as many parts as they have either way.
+constexpr long kLogprobTarget = 4;
 constexpr int kLogprobTickets = 1024;      // rows that may be cut: with more there is a workgroup for every compute unit anyway
 inline LogprobPlan logprob_plan(long rows, int vocab, int set, int cus) {
     const long sets = ((vocab + 14) / 8 + set - 1) / set, most = (sets + 3) / 4;

@@ -114,8 +114,8 @@ __global__ __launch_bounds__(256) void k_weigh(PagedWeigh c) {
 
 // The same for sequences whose rows fit NB blocks of 16 (decode steps, catch-ups): bound by the reading of K, so K comes as whole lines, through a ring of tiles of 32 keys in
 // LDS that is the wave's own (no barrier), with the exponents and with the weights as they were; the rows' queries stay in registers.  No joins: a position's weight is one wave's.
-// Few instructions a tile and four workgroups to a compute unit are what it takes to keep requests on their way: 64 sequences of 1024 to 16384 8-bit keys, 40 query heads, 113 us
-// (5.35 TB/s; 141 with two workgroups and rings of 16 KB, 267 with loads in the products' operand layout and no ring); one sequence of 8191 bf16 keys, 32 heads, 5.5 us.
+// All tiles of a sequence are gone through, with a window too.  Few instructions a tile and four workgroups to a compute unit are what it takes to keep requests on their way: 64
+// sequences of 1024 to 16384 8-bit keys, 40 query heads, 113 us (5.35 TB/s; 141 with two workgroups and rings of 16 KB, 267 with loads in the products' operand layout and no ring); one sequence of 8191 bf16 keys, 32 heads, 5.5 us.
 template <typename CT, int HD, int NB>
 struct WeighWave {
     static constexpr bool F32 = sizeof(CT) == 4, F8 = sizeof(CT) == 1;
@@ -307,9 +307,12 @@ __global__ __launch_bounds__(256, (WeighWave<CT, HD, NB>::kBlocks)) void k_weigh
 //   S = Q K^T with 32x32x16 products: lane (n, hh) = (lane & 31, lane >> 5) gets key n's scores of rows 8 i + 4 hh + 0..3 of a tile, i = 0..3, and adds their
 //   exponentials up; the halves of the wave are added at the end.
 // The rows that see a tile of keys are cut into c.splits ranges; with more than one each leaves its sums for k_weigh_join.
-// A score takes an fma, an exponential (a quarter-rate instruction) and an addition, 24 cycles a wave beside 16 of products: 2048 rows after 6145 positions, 32 heads of 128, 170 us with the
-// join's 5 (716 Tflop/s), matrix cores 37 % busy, vector issue 62 % and the exponentials' further cycles on top.  The next tile's products between this one's exponentials
-// (registers for two waves to a SIMD instead of three) took 213 us, all of a tile's queries read before its products as long as this.
+// 2048 rows after 6145 positions, 32 heads of 128: 168 us with the join's 5 (725 Tflop/s).  By the counters a SIMD is busy for 41 cycles with the 64 scores of a wave's instruction: 16 of
+// them products, and 4.3 vector instructions besides (an fma, an exponential, an addition, the rest addresses, statistics and tile ends), 21 cycles at 4 each and 8 for the exponential
+// (measured alone: 8.2 an exponential, 2.5 an fma with two waves and more).  16 and 21 are nine tenths of 41: the two hardly overlap; matrix cores are busy for 38 %, vector issue, the
+// products' own included, for 55 %.
+// The next tile's products between this one's exponentials (registers for two waves to a SIMD instead of three) took 213 us, all of a tile's queries read before its products as
+// long as this.  Keys are loaded whether or not any row of the range sees them, and a sequence of few rows beside a long piece goes through here range by range.
 template <typename CT, int HD>
 __global__ __launch_bounds__(256, 2) void k_weigh_many(PagedWeigh c) {
     constexpr int KS = HD / 16, kRowBytes = HD * 2, kTileBytes = 32 * kRowBytes, kReq = kTileBytes / 4096;     // requests of 1 KB to a wave (HD 32: half a one)

@@ -1,6 +1,5 @@
 """The forms that large calls of the steps around attention take, each reached by its rule in csrc/paged_rules.hpp: four heads to a group of lanes in rotation and append (bf16 heads of 64
-and 128; the others stay with one, for many rows too), several tiles to
-a wave in weighing, wide and narrow workgroups that move in eviction.  Tolerances are those of test_gpu_steps."""
+and 128; the others stay with one, for many rows too), several tiles to a wave in weighing, wide and narrow workgroups that move in eviction.  Tolerances are those of test_gpu_steps."""
 import pytest
 import torch
 
