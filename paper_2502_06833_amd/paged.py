@@ -88,10 +88,20 @@ def _rows(name, t, cache, rows, heads) -> Rows:
     return Rows(t.data_ptr(), s[0], s[1])
 
 
+def _cross(rows, heads, row, head, dim):
+    """Whether two vectors of different rows and heads share an element: some multiple of one stride lies within `dim` of one of the other."""
+    for h in range(1, heads):
+        r = h * head // row
+        if (r < rows and h * head - r * row < dim) or (r + 1 < rows and (r + 1) * row - h * head < dim):
+            return True
+    return False
+
+
 def _outputs(name, t, cache, rows, heads) -> Rows:
     """The same for a tensor that is written: every vector needs a place of its own."""
     r = _rows(name, t, cache, rows, heads)
-    if (rows > 1 and r.row_stride < cache.head_dim) or (heads > 1 and r.head_stride < cache.head_dim):
+    row, head, dim = r.row_stride, r.head_stride, cache.head_dim
+    if (rows > 1 and row < dim) or (heads > 1 and head < dim) or (rows > 1 and heads > 1 and row < (heads - 1) * head + dim and _cross(rows, heads, row, head, dim)):
         raise ValueError(f"{name}: vectors that overlap (strides {t.stride()}) cannot be written")
     return r
 
