@@ -23,7 +23,7 @@ def lib(tmp_path_factory):
     bodies = re.findall(r"^__device__ __forceinline__ void sincos_\w+\(.*?^}\n", text, re.M | re.S)
     assert len(bodies) == 2
     (d / "s.cpp").write_text(PREFIX + "".join(bodies) + CALLS)
-    subprocess.run(["g++", "-O2", "-std=c++17", "-mfma", "-ffp-contract=off", "-shared", "-fPIC", "-o", str(d / "s.so"), str(d / "s.cpp")], check=True)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-ffp-contract=off", "-shared", "-fPIC", "-o", str(d / "s.so"), str(d / "s.cpp")], check=True)
     L = C.CDLL(str(d / "s.so"))
     L.quarters.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_long]
     L.angles.argtypes = [C.c_void_p, C.c_double, C.c_void_p, C.c_void_p, C.c_long]
